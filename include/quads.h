@@ -54,6 +54,10 @@ typedef int qd_status;
 
 #define QD_EPI_NONE   0   /* out[r][n] = bf16(alpha * acc)                    */
 #define QD_EPI_SWIGLU 1   /* out[r][j] = bf16(silu(g_j) * u_j), N = 2I         */
+#define QD_EPI_SWIGLU_FP8 2  /* the same, quantised to FP8 (moe_fp8_block_grouped_gemm) */
+
+#define QD_SCORE_SOFTMAX 0   /* scores of moe_route_scored_permute              */
+#define QD_SCORE_SIGMOID 1
 
 /*
  * An NVFP4 tensor: `groups` matrices of [rows][cols].  The struct itself is
@@ -337,6 +341,8 @@ qd_status nvfp4_pack_frag_scales(const qd_nvfp4 *w, uint8_t *out, void *stream);
  *   y[t][n] = bf16( sum_{s=0..k-1} topk_w[t][s] * z[inv_row[t][s]][n] ),
  * accumulated in f32 in slot order.
  *   z : bf16 [T*k][H]; y : bf16 [T][H]; 1 <= k <= 32, H % 8 == 0.
+ *   A slot with inv_row -1 (a dead token of moe_route_scored_permute) adds
+ *   nothing.
  * ------------------------------------------------------------------- */
 qd_status moe_unpermute_combine(const void *z, const int32_t *inv_row, const float *topk_w,
                                 int64_t T, int32_t k, int64_t H, void *y, void *stream);
@@ -384,6 +390,133 @@ qd_status qd_fp8_moe_layer_forward(const void *x, const float *logits, int64_t T
                                    const uint8_t *w13_codes, const float *w13_dec,
                                    const uint8_t *w2_codes, const float *w2_dec, void *y,
                                    void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------
+ * moe_route_scored_permute -- the router of MoE models that score experts
+ * apart from choosing them (a variant of the routing of moe_route_permute;
+ * Sec. 4.1's model leaves the router open):
+ *   s = softmax(logits) or sigmoid(logits) over the E experts, c = s + bias;
+ *   groups > 1: the experts are `groups` runs of E / groups; a group's score is
+ *   the sum of its group_sum (1 or 2) largest c, and only the top_groups best
+ *   groups take part (ties to the lower group);
+ *   the k largest c are chosen, in that order (ties to the lower expert);
+ *   weight = scale * s / (sum of s over the chosen) with renorm 1 (0 where
+ *   that sum is 0), scale * s with renorm 0.  bias enters the choice only.
+ * Scores, sums and comparisons are float64.  Without bias and groups the order is
+ * that of the logits; softmax scores are renormalised as a softmax over the
+ * chosen logits.
+ *   logits  : [T] rows of E elements of dtype (QD_DTYPE_BF16 or QD_DTYPE_F32), ld
+ *             elements apart (ld >= E).  -inf is an expert with score 0; a NaN is
+ *             chosen last (softmax: it makes the token's weights NaN), and the
+ *             experts of a token are distinct and in range whatever the logits.
+ *   scoring : QD_SCORE_SOFTMAX or QD_SCORE_SIGMOID.
+ *   bias    : f32 [E], or NULL.
+ *   live    : uint8 [T], or NULL (every token is live).  A token with 0 takes no
+ *             expert: topk_ids -1, topk_w 0, inv_row -1 in its k slots.
+ *   topk_ids, topk_w, expert_offsets, row_token, inv_row : as
+ *             moe_route_permute; rows from expert_offsets[E] on (there are k for
+ *             each token that is not live) have row_token -1.
+ *   1 <= k <= 32, k <= top_groups * (E / groups), E <= 1024, groups <= 64,
+ *   E % groups == 0, scale finite.
+ * ------------------------------------------------------------------- */
+size_t    moe_route_scored_workspace(int64_t T, int32_t E, int32_t k);
+qd_status moe_route_scored_permute(const void *logits, int32_t dtype, int64_t ld, int64_t T,
+                                   int32_t E, int32_t k, int32_t scoring, const float *bias,
+                                   int32_t groups, int32_t top_groups, int32_t group_sum,
+                                   int32_t renorm, float scale, const uint8_t *live,
+                                   int32_t *topk_ids, float *topk_w, int32_t *expert_offsets,
+                                   int32_t *row_token, int32_t *inv_row, void *ws,
+                                   size_t ws_bytes, void *stream);
+
+/* moe_route_scored_backward -- the gradient of the logits from that of topk_w (the
+ * choice is constant): with g = scale * grad_w and q = s / (sum of s over the chosen),
+ *   sigmoid, renorm:  dl_j = q_j (g_j - sum_i g_i q_i) (1 - s_j)   at the chosen
+ *   sigmoid:          dl_j = g_j s_j (1 - s_j)                     at the chosen
+ *   softmax, renorm:  dl_j = q_j (g_j - sum_i g_i q_i)             at the chosen
+ *   softmax:          dl_e = s_e (g_e - sum_i g_i s_i)             at every expert
+ * and 0 elsewhere (g_e is 0 for an expert not chosen).  float64, rounded once.
+ *   topk_ids    : from moe_route_scored_permute; a slot with -1 has no gradient.
+ *   grad_w      : f32 [T][k].
+ *   grad_logits : [T] rows of E elements of dtype, ld_grad elements apart; written. */
+qd_status moe_route_scored_backward(const void *logits, int32_t dtype, int64_t ld, int64_t T,
+                                    int32_t E, int32_t k, int32_t scoring, int32_t renorm,
+                                    float scale, const int32_t *topk_ids, const float *grad_w,
+                                    void *grad_logits, int64_t ld_grad, void *stream);
+
+/* ---------------------------------------------------------------------
+ * FP8 with fine-grained scales (Sec. 2.2 "FP8" paragraph, the scales of the FP8
+ * rollout the paper compares against): E4M3 codes with one f32 scale for 128
+ * consecutive elements of an activation row, or for a 128 x 128 block of a weight
+ * matrix.  For a block with m = max |x| >= 2^-100, enc = 448 / m, dec = 1 / enc (f32);
+ * a smaller one takes enc = dec = 1; code = E4M3_RNE(clamp(x * enc, -448, 448)) with
+ * the sign in bit 7, and the element stands for code * dec.  A NaN keeps its place; an
+ * infinity makes every element of its block stand for NaN.  The last block of a row
+ * or matrix may be short.
+ *
+ * fp8_block_quantize_act
+ *   x      : [rows] rows of cols elements (bf16 or f32), ld elements apart;
+ *            cols % 16 == 0, ld >= cols, ld % 8 == 0.
+ *   codes  : u8 [rows][cols].
+ *   scales : f32 [ceil(cols / 128)][rows]: a block column's scales side by side.
+ *
+ * fp8_block_quantize_weight
+ *   w        : [groups][rows][cols] bf16 or f32, cols % 16 == 0.
+ *   codes    : u8 [groups][rows][cols].
+ *   scales   : f32 [groups][ceil(rows / 128)][ceil(cols / 128)].
+ *   codes_t, scales_t : NULL, or the same bank transposed, u8 [groups][cols][rows]
+ *              and f32 [groups][ceil(cols / 128)][ceil(rows / 128)], written in the
+ *              same pass (rows % 16 == 0): with it moe_fp8_block_grouped_gemm
+ *              gives the gradient of its activations, dx = dy w.
+ * ------------------------------------------------------------------- */
+qd_status fp8_block_quantize_act(const void *x, int32_t dtype, int64_t rows, int64_t cols,
+                                 int64_t ld, uint8_t *codes, float *scales, void *stream);
+qd_status fp8_block_quantize_weight(const void *w, int32_t dtype, int64_t groups, int64_t rows,
+                                    int64_t cols, uint8_t *codes, float *scales,
+                                    uint8_t *codes_t, float *scales_t, void *stream);
+
+/* ---------------------------------------------------------------------
+ * moe_fp8_block_grouped_gemm -- per expert e and grouped row r, over the blocks b of
+ * 128 elements of K:
+ *   v[r][n] = sum_b a_scales[b][src(r)] w_scales[e][n / 128][b]
+ *                   sum_{k in b} a[src(r)][k] w[e][n][k]
+ * (E4M3 products exact; the products of 64 elements are summed by one f8f6f4 MFMA,
+ * everything else is f32).
+ *   a_codes, a_scales : u8 [a_rows][K], f32 [ceil(K / 128)][a_rows];  row_token (values
+ *                     in [0, a_rows) below expert_offsets[E]) and expert_offsets as in
+ *                     moe_w4a4_grouped_gemm.
+ *   w_codes, w_scales : u8 [E][N][K], f32 [E][ceil(N / 128)][ceil(K / 128)].
+ *   epilogue        : QD_EPI_NONE: out bf16 [rows][N], N % 8 == 0;
+ *                     QD_EPI_SWIGLU: N = 2I, I % 32 == 0, gate rows [0, I), up rows
+ *                     [I, 2I); out bf16 [rows][I] = bf16(silu(g) * u);
+ *                     QD_EPI_SWIGLU_FP8: the f32 silu(g) * u quantised as by
+ *                     fp8_block_quantize_act: out u8 [rows][I], out_scales f32
+ *                     [ceil(I / 128)][rows].
+ *   out_scales      : QD_EPI_SWIGLU_FP8 only (ignored otherwise, NULL allowed).
+ * K % 16 == 0, E <= 1024; activation codes and one expert's weights below 4 GiB
+ * (otherwise QD_ERR_UNSUPPORTED).  Rows from expert_offsets[E] on are left as they were.
+ * ------------------------------------------------------------------- */
+qd_status moe_fp8_block_grouped_gemm(const uint8_t *a_codes, const float *a_scales,
+                                     int64_t a_rows, const int32_t *row_token,
+                                     const int32_t *expert_offsets, int32_t E, int64_t rows,
+                                     const uint8_t *w_codes, const float *w_scales, int64_t N,
+                                     int64_t K, int32_t epilogue, void *out, float *out_scales,
+                                     void *stream);
+
+/* qd_fp8_block_moe_layer_forward -- the FP8 layer with fine-grained scales: scored
+ * routing, x quantised per 1 x 128, W13 with SwiGLU and the quantisation of h, W2, combine:
+ * y bf16 [T][H].  x: bf16 [T][H]; logits: f32 [T][E]; w13: [E][2I][H] codes and their
+ * scales, w2: [E][H][I] (from fp8_block_quantize_weight); the routing arguments as
+ * moe_route_scored_permute (a token that is not live gets y = 0).  H % 16 == 0,
+ * I % 32 == 0.  The same results as its calls one after the other, bit for bit. */
+size_t    qd_fp8_block_moe_layer_workspace(int64_t T, int64_t H, int32_t E, int32_t k, int64_t I);
+qd_status qd_fp8_block_moe_layer_forward(const void *x, const float *logits, int64_t T, int64_t H,
+                                         int32_t E, int32_t k, int64_t I, int32_t scoring,
+                                         const float *bias, int32_t groups, int32_t top_groups,
+                                         int32_t group_sum, int32_t renorm, float scale,
+                                         const uint8_t *live, const uint8_t *w13_codes,
+                                         const float *w13_scales, const uint8_t *w2_codes,
+                                         const float *w2_scales, void *y, void *ws,
+                                         size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------
  * MXFP4 W4A4 comparison layer: the OCP Microscaling FP4 format that CDNA4's

@@ -28,7 +28,8 @@ __global__ __launch_bounds__(256) void combine_kernel(const uint16_t *__restrict
   for (int64_t t = blockIdx.y; t < T; t += gridDim.y) {
     if (t != blockIdx.y) __syncthreads();   // the previous token's rows are read
     if (threadIdx.x < k) {
-      srow[threadIdx.x] = (int64_t)inv_row[t * k + threadIdx.x] * H;
+      const int64_t row = inv_row[t * k + threadIdx.x];
+      srow[threadIdx.x] = row < 0 ? -1 : row * H;        // -1: a slot without a row
       sw[threadIdx.x] = wts[t * k + threadIdx.x];
     }
     __syncthreads();
@@ -48,12 +49,13 @@ __global__ __launch_bounds__(256) void combine_kernel(const uint16_t *__restrict
       uint4 v[8];
 #pragma unroll
       for (int s = 0; s < 8; ++s)
-        if (s < k) v[s] = reinterpret_cast<const uint4 *>(z + srow[s])[c];
+        if (s < k && srow[s] >= 0) v[s] = reinterpret_cast<const uint4 *>(z + srow[s])[c];
 #pragma unroll
       for (int s = 0; s < 8; ++s)
-        if (s < k) add(v[s], sw[s]);
+        if (s < k && srow[s] >= 0) add(v[s], sw[s]);
     } else {
-      for (int s = 0; s < k; ++s) add(reinterpret_cast<const uint4 *>(z + srow[s])[c], sw[s]);
+      for (int s = 0; s < k; ++s)
+        if (srow[s] >= 0) add(reinterpret_cast<const uint4 *>(z + srow[s])[c], sw[s]);
     }
     uint32_t o[4];
 #pragma unroll

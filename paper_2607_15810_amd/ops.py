@@ -508,6 +508,225 @@ class FP8MoELayer:
         return y
 
 
+# ---------------------------------------------------------------- scored routing
+
+_SCORING = {"softmax": Q.QD_SCORE_SOFTMAX, "sigmoid": Q.QD_SCORE_SIGMOID}
+_EPILOGUES = {None: Q.QD_EPI_NONE, "none": Q.QD_EPI_NONE, "swiglu": Q.QD_EPI_SWIGLU,
+              "swiglu_quant": Q.QD_EPI_SWIGLU_FP8}
+
+
+def _need(t, name, dtypes, shape, device=None):
+    """A tensor argument: on the GPU (that of the others), of one of the types and of
+    the shape (None: any extent), its rows without gaps."""
+    _require_cuda(t)
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
+    return t
+
+
+def _rows_of(t, name):
+    """(pointer, row stride) of a matrix whose rows are contiguous."""
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _dense(t, name):
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _dtype(t):
+    return Q.QD_DTYPE_BF16 if t.dtype == torch.bfloat16 else Q.QD_DTYPE_F32
+
+
+def _scoring(name):
+    if name not in _SCORING:
+        raise ValueError(f"scoring must be one of {sorted(_SCORING)}, not {name!r}")
+    return _SCORING[name]
+
+
+def _router_tensors(bias, live, E, T, dev):
+    if bias is not None:
+        _dense(_need(bias, "bias", (torch.float32,), (E,), dev), "bias")
+    if live is not None:
+        _dense(_need(live, "live", (torch.uint8, torch.bool), (T,), dev), "live")
+
+
+def route_scored(logits, k, scoring="softmax", bias=None, groups=1, top_groups=1, group_sum=1,
+                 renorm=True, scale=1.0, live=None):
+    """Scored routing (moe_route_scored_permute) of logits [T][E] (bf16 or f32, rows
+    contiguous): softmax or sigmoid scores; a bias [E] (f32) that enters the choice
+    only; the top_groups best of `groups` expert groups by the sum of their group_sum
+    best; weights renormalised over the chosen and times scale.  live (uint8 or bool
+    [T]): tokens with 0 take no expert.  Returns (ids, w, offsets, row_token, inv_row)."""
+    _need(logits, "logits", (torch.bfloat16, torch.float32), (None, None))
+    T, E = logits.shape
+    dev = logits.device
+    _router_tensors(bias, live, E, T, dev)
+    with torch.cuda.device(dev):
+        ptr, ld = _rows_of(logits, "logits")
+        ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+        w = torch.empty((T, k), dtype=torch.float32, device=dev)
+        offs = torch.empty(E + 1, dtype=torch.int32, device=dev)
+        row_token = torch.empty(T * k, dtype=torch.int32, device=dev)
+        inv_row = torch.empty((T, k), dtype=torch.int32, device=dev)
+        ws = _ws(Q.lib().moe_route_scored_workspace(T, E, k), dev)
+        Q.call("moe_route_scored_permute", ptr, _dtype(logits), ld, T, E, k, _scoring(scoring),
+               _ptr(bias), groups, top_groups, group_sum, int(renorm), float(scale), _ptr(live),
+               ids.data_ptr(), w.data_ptr(), offs.data_ptr(), row_token.data_ptr(),
+               inv_row.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+    return ids, w, offs, row_token, inv_row
+
+
+def route_scored_backward(logits, ids, grad_w, scoring="softmax", renorm=True, scale=1.0):
+    """The gradient of route_scored's logits (their type) from that of its weights
+    (grad_w f32 [T][k]); ids as route_scored returned them."""
+    _need(logits, "logits", (torch.bfloat16, torch.float32), (None, None))
+    T, E = logits.shape
+    dev = logits.device
+    k = ids.shape[-1]
+    _dense(_need(ids, "ids", (torch.int32,), (T, k), dev), "ids")
+    _dense(_need(grad_w, "grad_w", (torch.float32,), (T, k), dev), "grad_w")
+    with torch.cuda.device(dev):
+        ptr, ld = _rows_of(logits, "logits")
+        grad = torch.empty((T, E), dtype=logits.dtype, device=dev)
+        Q.call("moe_route_scored_backward", ptr, _dtype(logits), ld, T, E, k, _scoring(scoring),
+               int(renorm), float(scale), ids.data_ptr(), grad_w.data_ptr(), grad.data_ptr(), E,
+               _stream())
+    return grad
+
+
+# ---------------------------------------------------------------- FP8 with block scales
+
+def _blocks(n):
+    return (n + 127) // 128
+
+
+def fp8_block_quantize_act(x):
+    """E4M3 codes with one f32 scale per 128 elements of a row of x ([rows][cols] bf16
+    or f32, rows contiguous; cols % 16 == 0).  Returns (codes u8 [rows][cols],
+    scales [ceil(cols / 128)][rows])."""
+    _need(x, "x", (torch.bfloat16, torch.float32), (None, None))
+    rows, cols = x.shape
+    with torch.cuda.device(x.device):
+        ptr, ld = _rows_of(x, "x")
+        codes = torch.empty((rows, cols), dtype=torch.uint8, device=x.device)
+        scales = torch.empty((_blocks(cols), rows), dtype=torch.float32, device=x.device)
+        Q.call("fp8_block_quantize_act", ptr, _dtype(x), rows, cols, ld, codes.data_ptr(),
+               scales.data_ptr(), _stream())
+    return codes, scales
+
+
+def fp8_block_quantize_weight(w, transposed=False):
+    """E4M3 codes with one f32 scale per 128 x 128 block of w ([E][N][K] bf16 or f32).
+    Returns (codes u8 [E][N][K], scales [E][ceil(N / 128)][ceil(K / 128)]) and, with
+    transposed, the same bank as [E][K][N] (N % 16 == 0), which gives input gradients:
+    (codes, scales, codes_t, scales_t)."""
+    _need(w, "w", (torch.bfloat16, torch.float32), (None, None, None))
+    dev = w.device
+    E, N, K = w.shape
+    with torch.cuda.device(dev):
+        codes = torch.empty((E, N, K), dtype=torch.uint8, device=dev)
+        scales = torch.empty((E, _blocks(N), _blocks(K)), dtype=torch.float32, device=dev)
+        ct = st = None
+        if transposed:
+            ct = torch.empty((E, K, N), dtype=torch.uint8, device=dev)
+            st = torch.empty((E, _blocks(K), _blocks(N)), dtype=torch.float32, device=dev)
+        Q.call("fp8_block_quantize_weight", _dense(w, "w"), _dtype(w), E, N, K, codes.data_ptr(),
+               scales.data_ptr(), _ptr(ct), _ptr(st), _stream())
+    return (codes, scales, ct, st) if transposed else (codes, scales)
+
+
+def _block_bank(codes, scales, name, dev=None):
+    _need(codes, name, (torch.uint8,), (None, None, None), dev)
+    E, N, K = codes.shape
+    _need(scales, name + " scales", (torch.float32,), (E, _blocks(N), _blocks(K)), codes.device)
+    return _dense(codes, name), _dense(scales, name + " scales")
+
+
+def fp8_block_grouped_gemm(a_codes, a_scales, w_codes, w_scales, rows, row_token=None,
+                           offsets=None, epilogue=None):
+    """The grouped product of block-scaled operands (moe_fp8_block_grouped_gemm).
+    epilogue None: bf16 [rows][N]; "swiglu": bf16 [rows][N / 2]; "swiglu_quant": (codes
+    [rows][N / 2], scales), quantised as fp8_block_quantize_act does.  Rows from
+    offsets[E] on are left as the allocation gave them."""
+    if epilogue not in _EPILOGUES:
+        raise ValueError(f"epilogue must be one of {list(_EPILOGUES)}, not {epilogue!r}")
+    _need(a_codes, "a_codes", (torch.uint8,), (None, None))
+    dev = a_codes.device
+    a_rows, K = a_codes.shape
+    _need(a_scales, "a_scales", (torch.float32,), (_blocks(K), a_rows), dev)
+    wp, sp = _block_bank(w_codes, w_scales, "w_codes", dev)
+    E, N = w_codes.shape[:2]
+    if w_codes.shape[2] != K:
+        raise ValueError(f"w_codes has K = {w_codes.shape[2]}, a_codes {K}")
+    if row_token is not None:
+        _need(row_token, "row_token", (torch.int32,), (None,), dev)
+        if row_token.numel() < rows:
+            raise ValueError("row_token has fewer than `rows` entries")
+        _dense(row_token, "row_token")
+    if offsets is not None:
+        _dense(_need(offsets, "offsets", (torch.int32,), (E + 1,), dev), "offsets")
+    epi = _EPILOGUES[epilogue]
+    with torch.cuda.device(dev):
+        cols = N if epi == Q.QD_EPI_NONE else N // 2
+        fp8 = epi == Q.QD_EPI_SWIGLU_FP8
+        out = torch.empty((rows, cols), dtype=torch.uint8 if fp8 else torch.bfloat16, device=dev)
+        scales = None
+        if fp8:
+            scales = torch.empty((_blocks(cols), rows), dtype=torch.float32, device=dev)
+        Q.call("moe_fp8_block_grouped_gemm", _dense(a_codes, "a_codes"),
+               _dense(a_scales, "a_scales"), a_rows, _ptr(row_token), _ptr(offsets), E, rows, wp,
+               sp, N, K, epi, out.data_ptr(), _ptr(scales), _stream())
+    return (out, scales) if fp8 else out
+
+
+class FP8BlockMoELayer:
+    """The FP8 layer with block scales and scored routing through
+    qd_fp8_block_moe_layer_forward, with a reusable workspace (calls on it must follow
+    one another: one stream, or ordered by events).  w13 [E][2I][H], w2 [E][H][I] from
+    fp8_block_quantize_weight; the routing arguments as route_scored."""
+
+    def __init__(self, w13_codes, w13_scales, w2_codes, w2_scales, T, k, scoring="softmax",
+                 bias=None, groups=1, top_groups=1, group_sum=1, renorm=True, scale=1.0):
+        self.device = w13_codes.device
+        self._w13 = _block_bank(w13_codes, w13_scales, "w13_codes")
+        self._w2 = _block_bank(w2_codes, w2_scales, "w2_codes", self.device)
+        self.E, N13, self.H = w13_codes.shape
+        self.I = N13 // 2
+        if N13 % 2 or tuple(w2_codes.shape) != (self.E, self.H, self.I):
+            raise ValueError("w13_codes must be [E][2I][H] and w2_codes [E][H][I]")
+        _router_tensors(bias, None, self.E, T, self.device)
+        self._keep = (w13_codes, w13_scales, w2_codes, w2_scales, bias)
+        self.T, self.k = T, k
+        self._route = (_scoring(scoring), _ptr(bias), groups, top_groups, group_sum, int(renorm),
+                       float(scale))
+        n = Q.lib().qd_fp8_block_moe_layer_workspace(T, self.H, self.E, k, self.I)
+        self.ws = _ws(n, self.device)
+
+    def __call__(self, x, logits, live=None, y=None):
+        """x bf16 [T][H], logits f32 [T][E], live as route_scored; y bf16 [T][H]."""
+        T, H, E, dev = self.T, self.H, self.E, self.device
+        _dense(_need(x, "x", (torch.bfloat16,), (T, H), dev), "x")
+        _dense(_need(logits, "logits", (torch.float32,), (T, E), dev), "logits")
+        _router_tensors(None, live, E, T, dev)
+        with torch.cuda.device(dev):
+            if y is None:
+                y = torch.empty((T, H), dtype=torch.bfloat16, device=dev)
+            else:
+                _dense(_need(y, "y", (torch.bfloat16,), (T, H), dev), "y")
+            Q.call("qd_fp8_block_moe_layer_forward", x.data_ptr(), logits.data_ptr(), T, H, E,
+                   self.k, self.I, *self._route, _ptr(live), *self._w13, *self._w2, y.data_ptr(),
+                   self.ws.data_ptr(), self.ws.numel(), _stream())
+        return y
+
+
 def mxfp4_quantize_rows(x):
     """MXFP4 codes and E8M0 block scales of x ([..][cols] bf16 or f32,
     cols % 32 == 0; a weight bank [E][N][K] is E*N rows).  Returns

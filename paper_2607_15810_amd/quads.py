@@ -24,6 +24,9 @@ QD_DTYPE_BF16 = 0
 QD_DTYPE_F32 = 1
 QD_EPI_NONE = 0
 QD_EPI_SWIGLU = 1
+QD_EPI_SWIGLU_FP8 = 2
+QD_SCORE_SOFTMAX = 0
+QD_SCORE_SIGMOID = 1
 
 STAGE_NAMES = ["route", "quant_x", "select", "w13", "quant_h", "w2", "combine"]
 
@@ -95,6 +98,27 @@ SIGNATURES = {
     "qd_fp8_moe_layer_forward": (c_int, [c_void_p, c_void_p, c_int64, c_int64, c_int32, c_int32,
                                          c_int64, c_int32, c_void_p, c_void_p, c_void_p,
                                          c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "moe_route_scored_workspace": (c_size_t, [c_int64, c_int32, c_int32]),
+    "moe_route_scored_permute": (c_int, [c_void_p, c_int32, c_int64, c_int64, c_int32, c_int32,
+                                         c_int32, c_void_p, c_int32, c_int32, c_int32, c_int32,
+                                         c_float, c_void_p, c_void_p, c_void_p, c_void_p,
+                                         c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "moe_route_scored_backward": (c_int, [c_void_p, c_int32, c_int64, c_int64, c_int32, c_int32,
+                                          c_int32, c_int32, c_float, c_void_p, c_void_p,
+                                          c_void_p, c_int64, c_void_p]),
+    "fp8_block_quantize_act": (c_int, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p,
+                                       c_void_p, c_void_p]),
+    "fp8_block_quantize_weight": (c_int, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p,
+                                          c_void_p, c_void_p, c_void_p, c_void_p]),
+    "moe_fp8_block_grouped_gemm": (c_int, [c_void_p, c_void_p, c_int64, c_void_p, c_void_p,
+                                           c_int32, c_int64, c_void_p, c_void_p, c_int64, c_int64,
+                                           c_int32, c_void_p, c_void_p, c_void_p]),
+    "qd_fp8_block_moe_layer_workspace": (c_size_t, [c_int64, c_int64, c_int32, c_int32, c_int64]),
+    "qd_fp8_block_moe_layer_forward": (c_int, [c_void_p, c_void_p, c_int64, c_int64, c_int32,
+                                               c_int32, c_int64, c_int32, c_void_p, c_int32,
+                                               c_int32, c_int32, c_int32, c_float, c_void_p,
+                                               c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                               c_void_p, c_size_t, c_void_p]),
     "mxfp4_quantize_rows": (c_int, [c_void_p, c_int32, c_int64, c_int64, c_void_p, c_void_p,
                                     c_void_p]),
     "moe_mxfp4_grouped_gemm": (c_int, [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int32,

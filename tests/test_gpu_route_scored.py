@@ -1,0 +1,173 @@
+"""Scored routing and its gradient on the GPU against the float64 oracle.
+
+Choices and permutations must be equal (both sides compare float64 scores; equal
+logits give equal scores on each side).  A weight is float64 rounded once to float32:
+2^-24 of it.  A gradient in float32 likewise, in bf16 2^-8; the float64 arithmetic
+before that rounding is off by less than 2^-40 of its terms."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import fp8_block as OB
+from paper_2607_15810_amd import ops
+from paper_2607_15810_amd import quads as Q
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    Q.lib()
+    yield
+
+
+def np_of(t):
+    return t.detach().cpu().numpy()
+
+
+def check(got, ref):
+    ids, w, offs, tok, inv = [np_of(t) for t in got]
+    assert np.array_equal(ids, ref["ids"])
+    assert np.array_equal(offs, ref["offsets"])
+    assert np.array_equal(tok, ref["row_token"])
+    assert np.array_equal(inv, ref["inv_row"])
+    d = np.abs(w.astype(np.float64) - ref["w"])
+    assert (d <= ref["w"] * 2.0 ** -23.99 + 2.0 ** -149).all(), d.max()
+
+
+CASES = [
+    # T, E, k, router
+    (1, 1, 1, dict()),
+    (1, 8, 8, dict(scoring="sigmoid")),
+    (1, 256, 8, dict(scoring="sigmoid", bias=True, groups=8, top_groups=4, group_sum=2, scale=2.5)),
+    (3, 60, 4, dict(renorm=False)),
+    (64, 128, 8, dict(bias=True)),
+    (65, 128, 6, dict(scoring="sigmoid", groups=4, top_groups=2, group_sum=1)),
+    (255, 160, 6, dict(bias=True, groups=8, top_groups=3, group_sum=2, scale=16.0, renorm=False)),
+    (256, 96, 8, dict(scoring="sigmoid", bias=True)),
+    (257, 256, 32, dict(scoring="sigmoid", bias=True, groups=64, top_groups=20, group_sum=2)),
+    (700, 64, 8, dict()),
+    (1025, 129, 3, dict(scoring="sigmoid", renorm=False)),
+    (300, 384, 8, dict(scoring="sigmoid", bias=True, groups=1)),
+    (70, 1024, 10, dict(bias=True, groups=16, top_groups=2, group_sum=2)),
+    (520, 513, 1, dict()),
+    (40, 24, 2, dict(scoring="sigmoid", bias=True, groups=24, top_groups=2, group_sum=1)),
+]
+
+
+@pytest.mark.parametrize("live", [None, "some", "none"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("case", CASES, ids=[f"t{c[0]}_e{c[1]}_k{c[2]}" for c in CASES])
+def test_route(case, dtype, live):
+    T, E, k, kw = case
+    kw = dict(kw)
+    rng = np.random.default_rng(T * 1000 + E)
+    # rows E + 3 apart; bf16 gives many equal logits
+    wide = torch.from_numpy(rng.standard_normal((T, E + 3)).astype(np.float32)).to(DEV).to(dtype)
+    lg = wide[:, :E]
+    if kw.pop("bias", False):
+        b = torch.from_numpy((0.1 * rng.standard_normal(E)).astype(np.float32))
+        kw["bias"] = b
+    lv = None
+    if live:
+        lv = (rng.random(T) < 0.6) if live == "some" else np.zeros(T, bool)
+    okw = dict(kw, bias=np_of(kw["bias"]) if "bias" in kw else None)
+    ref = OB.route(np_of(lg.float()), k, live=lv, **okw)
+    if "bias" in kw:
+        kw["bias"] = kw["bias"].to(DEV)
+    got = ops.route_scored(lg, k, live=None if lv is None else torch.from_numpy(lv).to(DEV), **kw)
+    check(got, ref)
+    # the gradient
+    gw = torch.from_numpy(rng.standard_normal((T, k)).astype(np.float32)).to(DEV)
+    sc, rn, sl = kw.get("scoring", "softmax"), kw.get("renorm", True), kw.get("scale", 1.0)
+    gr = ops.route_scored_backward(lg, got[0], gw, scoring=sc, renorm=rn, scale=sl)
+    assert gr.dtype == dtype
+    if T * E * E <= 2 ** 24:
+        d = OB.route_backward(np_of(lg.float()), ref["ids"], np_of(gw), sc, rn, sl)
+        half = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8 * (1 + 2.0 ** -15)
+        err = np.abs(np_of(gr.float()).astype(np.float64) - d)
+        assert (err <= half * np.abs(d) * 1.001 + abs(sl) * 2.0 ** -38).all()
+
+
+def test_ties_and_extremes():
+    E = 64
+    lg = torch.zeros((6, E), device=DEV)
+    lg[1, :] = -float("inf")                       # every expert masked
+    lg[2, 5:] = -float("inf")                      # fewer than k left
+    lg[3, 10] = lg[3, 40] = 90.0                   # saturated: sigmoid 1 twice
+    lg[4, :] = torch.finfo(torch.float32).min
+    lg[5, 33] = 1.0
+    for kw in (dict(), dict(scoring="sigmoid"), dict(renorm=False),
+               dict(scoring="sigmoid", groups=8, top_groups=2, group_sum=2)):
+        with np.errstate(over="ignore"):
+            ref = OB.route(np_of(lg), 8, **kw)
+        check(ops.route_scored(lg, 8, **kw), ref)
+
+
+def test_nan_stays_in_its_row():
+    rng = np.random.default_rng(3)
+    lg = torch.from_numpy(rng.standard_normal((9, 128)).astype(np.float32)).to(DEV)
+    clean = ops.route_scored(lg, 4, scoring="sigmoid", groups=4, top_groups=2)
+    bad = lg.clone()
+    bad[4, 7:] = float("nan")
+    for sc in ("sigmoid", "softmax"):
+        ids, w, offs, tok, inv = ops.route_scored(bad, 4, scoring=sc, groups=4, top_groups=2)
+        i = np_of(ids)
+        assert ((i >= 0) & (i < 128)).all() and all(len(set(r)) == 4 for r in i.tolist())
+        assert int(offs[-1]) == 36
+    ids = ops.route_scored(bad, 4, scoring="sigmoid", groups=4, top_groups=2)[0]
+    keep = [t for t in range(9) if t != 4]
+    assert torch.equal(ids[keep], clean[0][keep])
+    assert set(np_of(ids[4]).tolist()) <= set(range(0, 7)) | set(range(0, 128))
+
+
+def test_no_tokens():
+    ids, w, offs, tok, inv = ops.route_scored(torch.zeros((0, 8), device=DEV), 2)
+    assert ids.shape == (0, 2) and not offs.any()
+    g = ops.route_scored_backward(torch.zeros((0, 8), device=DEV), ids, w)
+    assert g.shape == (0, 8)
+
+
+def test_gradient_leaves_the_gaps_between_rows():
+    T, E, k, ld = 5, 24, 3, 40
+    lg = torch.randn((T, E), device=DEV)
+    ids = ops.route_scored(lg, k)[0]
+    gw = torch.randn((T, k), device=DEV)
+    out = torch.full((T, ld), 7.0, device=DEV)
+    Q.call("moe_route_scored_backward", lg.data_ptr(), Q.QD_DTYPE_F32, E, T, E, k, 0, 1, 1.0,
+           ids.data_ptr(), gw.data_ptr(), out.data_ptr(), ld,
+           torch.cuda.current_stream().cuda_stream)
+    assert (out[:, E:] == 7.0).all()
+    assert torch.equal(out[:, :E], ops.route_scored_backward(lg, ids, gw))
+
+
+def test_two_streams_and_a_graph():
+    T, E, k = 300, 128, 8
+    kw = dict(scoring="sigmoid", groups=8, top_groups=4, group_sum=2)
+    a, b = torch.randn((T, E), device=DEV), torch.randn((T, E), device=DEV)
+    want = [ops.route_scored(x, k, **kw) for x in (a, b)]
+    torch.cuda.synchronize()
+    got = []
+    for x in (a, b):
+        st = torch.cuda.Stream()
+        with torch.cuda.stream(st):
+            got.append(ops.route_scored(x, k, **kw))
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(p, q) for p, q in zip(g, w))
+    x = a.clone()
+    ops.route_scored(x, k, **kw)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ops.route_scored(x, k, **kw)
+    for src, w in ((b, want[1]), (a, want[0]), (b, want[1])):
+        x.copy_(src)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, w))
+        assert torch.equal(ops.route_scored(src, k, **kw)[0], w[0])
