@@ -2,21 +2,38 @@
 //   v[r][n] = sum_kb sa[kb][src(r)] sw[e][n / 128][kb] sum_{k in block kb} a[src(r)][k] w[e][n][k]
 // with its epilogues: bf16, SwiGLU in bf16, SwiGLU quantised to FP8 with 1 x 128 scales.
 //
-// A block's 128 products go through two v_mfma_scale_f32_32x32x64_f8f6f4 with unit
-// scales into a partial sum, which one multiply-add per element folds into the f32
-// total with the product of the two scales.  The weights are the instruction's first
-// operand, so a lane holds one activation row: its row scale is one register, the
-// weight scale is uniform, and four consecutive columns of a row leave a lane together.
+// Arithmetic.  The FP8 MFMAs add four products at a time and drop what lies more than
+// about twelve bits below the largest of them (measured against float64, K = 128: up to
+// 2^-12.5 of sum |products| from a 448 among values near 2^-4, on every fp8 and f8f6f4
+// shape), so a sum on them is no 32-bit sum.  Operands are decoded to f16 in registers
+// (v_cvt_scalef32_pk_f16_fp8, exact for every code) and multiplied on
+// v_mfma_f32_32x32x16_f16: 2^-22 on the same inputs, at the f16 rate.
+//
+// A block's 128 products go into a partial sum, which one multiply-add per element
+// folds into the f32 total with the product of the two scales.  The weights are the
+// instruction's first operand, so a lane holds one activation row: its row scale is one
+// register, the weight scale is uniform, and the columns of a row leave a lane together.
+//
+//  * Workgroup tile: up to 64 MF rows of one expert x 256 weight rows (SwiGLU: 128 gate
+//    rows and the matching up rows, one block of 128 of h), eight waves in a 2 x 4 grid of
+//    32 MF rows x 64 weight rows.  The schedule is the NVFP4 panel kernel's
+//    (panel_sched.h): one persistent workgroup per CU, its tiles' stages one stream
+//    through an LDS ring filled by direct global->LDS loads.
+//  * A stage is one block of K: 128 bytes of every row, the tile's row scales of that
+//    block and the scales of its weight fragments.  Pieces of 16 bytes past K come from a
+//    zero in memory.  The pieces of a row are placed by a row-dependent XOR, so the
+//    fragment reads are free of bank conflicts.  One barrier per stage.
 #include "fp8_block_dev.h"
 #include "lds_dma.h"
+#include "panel_sched.h"
 #include "tile_sched.h"
 
 namespace {
 
 using namespace qdb;
 using namespace qdl;
+using namespace qdp;
 
-typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct BlkArgs {
@@ -34,10 +51,16 @@ struct BlkArgs {
   float *out_scales;           // [N / 256 rounded up][rows]
 };
 
-constexpr int BK_EMAX = 1024;
+__device__ const uint4 bk_zero = {0, 0, 0, 0};
 
-__device__ __forceinline__ f32x16 mfma_f8(v8i a, v8i b, f32x16 c) {
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 127, 0, 127);
+__device__ __forceinline__ f16x2 dec2(uint32_t w, bool hi) {
+  return hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true)
+            : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false);
+}
+// eight codes (two words) to f16, exact
+__device__ __forceinline__ f16x8 dec8(uint32_t lo, uint32_t hi) {
+  const f16x2 a = dec2(lo, false), b = dec2(lo, true), c = dec2(hi, false), d = dec2(hi, true);
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 __device__ __forceinline__ float bk_swiglu(float g, float u) {
   const float ex = __builtin_amdgcn_exp2f(-g * 1.4426950408889634f);
@@ -48,113 +71,444 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   typedef float f2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
 }
+// The upper half of a against the lower half of b: with a and b the words of columns
+// 4 h .. and 16 + 4 h .. (h the lane's half) the two results are, for the lower lanes,
+// the words of columns 0 and 4, for the upper ones of 16 and 20.
+struct Pair32 { uint32_t x, y; };
+__device__ __forceinline__ Pair32 swap32(uint32_t a, uint32_t b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  return {r[0], r[1]};
+}
 
-// 32 rows of an expert x 256 weight rows (SwiGLU: 128 gate rows and the matching up
-// rows), four waves of two 32 x 32 fragments, operands straight from memory.
-template <int EPI>
-__global__ __launch_bounds__(256) void gemm_block_kernel(BlkArgs p, int ntn) {
-  __shared__ int sh_w[4], sh_t[4];
-  __shared__ float sh_m[4][32];
-  const int tid = threadIdx.x, lane = tid & 63, w = (int)uni((uint32_t)tid >> 6);
-  const qdt::Tile tl = qdt::find_tile<32>(p.offsets, p.E, p.rows, ntn, sh_w, sh_t);
-  if (tl.e < 0) return;
-  const int N = p.N, K = p.K, KB = (K + FB - 1) / FB, NB = (N + FB - 1) / FB;
-  const int c = lane & 31, h = lane >> 5;
+template <int MF>
+struct BkCfg {
+  static constexpr int M = 64 * MF;
+  static constexpr int BOFF = M * 128;                 // weight codes
+  static constexpr int SOFF = BOFF + 32768;            // row scales, then fragment scales
+  static constexpr int SLOT = SOFF + (MF + 1) * 256;
+  static constexpr int LPS = MF + 4 + 1;               // loads per wave and stage
+};
+
+struct BkLayout {
+  int tok, amax, dummy, offs, mpre, perm, total;
+};
+// after the ring: the tokens of two tiles, the waves' row maxima (quantising
+// epilogue), the target of placeholder loads, the tile schedule
+__host__ __device__ inline BkLayout bk_layout(int mf, int ns, int E) {
+  BkLayout L{};
+  int o = ns * (64 * mf * 128 + 32768 + (mf + 1) * 256);
+  auto take = [&](int bytes) { const int at = o; o += (bytes + 15) & ~15; return at; };
+  L.tok = take(2 * 64 * mf * 4);
+  L.amax = take(4 * 64 * mf * 4);
+  L.dummy = take(256);
+  L.offs = take((E + 1) * 4);
+  L.mpre = take((E + 1) * 4);
+  L.perm = take(E * 2);
+  L.total = o;
+  return L;
+}
+
+typedef const __attribute__((address_space(4))) BlkArgs *BkArgPtr;
+__device__ __forceinline__ BkArgPtr bk_args() {
+  BkArgPtr q = (BkArgPtr)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(q));
+  return q;
+}
+
+// 16-byte piece c of tile row r sits at piece c ^ bk_swz(r) of the row's 128
+__device__ __forceinline__ int bk_swz(int r) { return (r >> 1) & 7; }
+
+// weight row of the tile's row tb (0 past the last: never stored)
+template <bool GLU>
+__device__ __forceinline__ int bk_wrow(int tb, int nt, int N) {
+  if (GLU) {
+    const int I = N >> 1, c = nt * 128 + (tb & 127);
+    return c < I ? c + (tb < 128 ? 0 : I) : 0;
+  }
+  const int c = nt * PN_N + tb;
+  return c < N ? c : 0;
+}
+
+template <int MF, int EPI>
+__global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, PnDeal deal, int ns) {
+  using C = BkCfg<MF>;
   constexpr bool GLU = EPI != QD_EPI_NONE;
-  const int I = GLU ? N >> 1 : N;
-  int64_t src = tl.row0 + (c < tl.nrows ? c : 0);
-  if (p.row_token) src = p.row_token[src];
-  const uint8_t *pa = p.a + src * K;
-  const uint8_t *pw[2];
-  const float *ws[2];
-  int col0[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    col0[j] = GLU ? tl.nt * 128 + 32 * w : tl.nt * 256 + 64 * w + 32 * j;
-    const int wr = (GLU && j == 1 ? I : 0);
-    const int n = wr + (col0[j] + c < I ? col0[j] + c : 0);
-    pw[j] = p.w + ((int64_t)tl.e * N + n) * K;
-    const int nb = col0[j] < I ? (wr + col0[j]) / FB : 0;
-    ws[j] = p.w_scales + ((int64_t)tl.e * NB + nb) * KB;
-  }
-  auto piece = [&](const uint8_t *q, int k) __attribute__((always_inline)) -> uint4 {
-    return k < K ? *reinterpret_cast<const uint4 *>(q + k) : make_uint4(0, 0, 0, 0);
+  extern __shared__ __align__(16) unsigned char lds[];
+  __shared__ int sh_w[8];
+  __shared__ int sh_c[8][2 * MF + 1];
+  const int tid = threadIdx.x, lane = tid & 63, w = (int)uni((uint32_t)tid >> 6);
+  const int N = p.N, E = p.E, K = p.K;
+  const int KB = (K + FB - 1) / FB, NB = (N + FB - 1) / FB;
+  const int nst = KB > 2 ? KB : 2;             // two stages at least (zeros past K)
+  const BkLayout L = bk_layout(MF, ns, E);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  int32_t *offs = reinterpret_cast<int32_t *>(lds + L.offs);
+  int32_t *mpre = reinterpret_cast<int32_t *>(lds + L.mpre);
+  uint16_t *perm = reinterpret_cast<uint16_t *>(lds + L.perm);
+  const int32_t *tokb = reinterpret_cast<const int32_t *>(lds + L.tok);
+  float *amax = reinterpret_cast<float *>(lds + L.amax);
+  pn_schedule<MF>(p.offsets, p.rows, E, offs, mpre, perm, sh_w, sh_c);
+  __syncthreads();
+  const PnSched S{offs, mpre, perm, E, deal, (int)(blockIdx.x & 7)};
+  const int nsl = gridDim.x >> 3;
+  const int t_end = pn_walk(S);
+  int ct = blockIdx.x >> 3;                // the tile being multiplied
+  // two waves of a SIMD (w, w + 4) take different row halves
+  const int wm = (w ^ (w >> 2)) & 1, wn = w >> 1;
+
+  // ---- loads.  A line load: 8 rows, lane l brings row l / 8's piece
+  // (l % 8) ^ swz (rows 8 (w + 8 j) ..: the XOR depends on w's parity only)
+  const uint32_t pc = 16u * (uint32_t)((lane & 7) ^ bk_swz(8 * (w & 1) + (lane >> 3)));
+  const uint32_t dummy = lds0 + (uint32_t)L.dummy;
+  int it = ct, left = 0, ecur = 0, ibuf = 0;
+  PnTile itl{}, nx{};
+  uint32_t oa[MF], ob[4], os = 0;
+  const uint8_t *pa = nullptr, *wb = nullptr, *sb = nullptr;
+  auto tok_dma = [&](const PnTile &tl, int buf) __attribute__((always_inline)) {
+    const int32_t *rt = bk_args()->row_token;
+    const int wi = pn_fresh_s(w);
+    if (rt && wi < MF) {
+      const int r = 64 * wi + lane;
+      dma4s(uni_ptr(rt), (uint32_t)(tl.row0 + (r < tl.nrows ? r : 0)) * 4u,
+            uni(lds0 + (uint32_t)(L.tok + buf * (C::M * 4) + wi * 256)));
+    }
   };
-  struct Two { uint4 x, y; };
-  f32x16 acc[2];
+  auto src = [&](const int32_t *rt, int r) __attribute__((always_inline)) -> uint32_t {
+    if (rt) return (uint32_t)tokb[ibuf * C::M + r];
+    return (uint32_t)(itl.row0 + (r < itl.nrows ? r : 0));
+  };
+  // to tile itl's first stage (its tokens are in LDS), the tokens of the tile
+  // after it on their way
+  auto bind = [&]() __attribute__((always_inline)) {
+    const BkArgPtr q = bk_args();
+    const int wi = pn_fresh_s(w), ln = pn_fresh(lane);
+    wb = uni_ptr(q->w + (int64_t)itl.e * N * K);
+    pa = uni_ptr(q->a);
+    const int32_t *rt = q->row_token;
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < MF; ++j)
+      oa[j] = src(rt, 8 * (wi + 8 * j) + (ln >> 3)) * (uint32_t)K + pc;
 #pragma unroll
-    for (int q = 0; q < 16; ++q) acc[j][q] = 0.0f;
-  for (int kb = 0; kb < KB; ++kb) {
-    const float sa = p.a_scales[(int64_t)kb * p.a_rows + src];
-    v8i a[2];
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      const int k = kb * FB + 64 * st + 32 * h;
-      a[st] = __builtin_bit_cast(v8i, Two{piece(pa, k), piece(pa, k + 16)});
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      f32x16 part;
-#pragma unroll
-      for (int q = 0; q < 16; ++q) part[q] = 0.0f;
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        const int k = kb * FB + 64 * st + 32 * h;
-        part = mfma_f8(__builtin_bit_cast(v8i, Two{piece(pw[j], k), piece(pw[j], k + 16)}), a[st], part);
-      }
-      const float s = sa * ws[j][kb];
-#pragma unroll
-      for (int q = 0; q < 16; ++q) acc[j][q] = __builtin_fmaf(part[q], s, acc[j][q]);
-    }
-  }
-  // element q of a fragment: column 8 (q / 4) + 4 h + q % 4 of row c
-  const int64_t row = tl.row0 + c;
-  const bool in_row = c < tl.nrows;
-  if constexpr (!GLU) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int q = 0; q < 16; q += 4) {
-        const int n = col0[j] + 2 * q + 4 * h;
-        if (in_row && n < N)
-          *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + row * N + n) = make_uint2(
-              bf16_pair(acc[j][q], acc[j][q + 1]), bf16_pair(acc[j][q + 2], acc[j][q + 3]));
-      }
-  } else {
-    float v[16];
-#pragma unroll
-    for (int q = 0; q < 16; ++q) v[q] = bk_swiglu(acc[0][q], acc[1][q]);
-    if constexpr (EPI == QD_EPI_SWIGLU) {
-#pragma unroll
-      for (int q = 0; q < 16; q += 4) {
-        const int n = col0[0] + 2 * q + 4 * h;
-        if (in_row && n < I)
-          *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + row * I + n) =
-              make_uint2(bf16_pair(v[q], v[q + 1]), bf16_pair(v[q + 2], v[q + 3]));
-      }
+    for (int j = 0; j < 4; ++j)
+      ob[j] = (uint32_t)bk_wrow<GLU>(8 * (wi + 8 * j) + (ln >> 3), itl.nt, N) * (uint32_t)K + pc;
+    // the stage's scales: rows of the tile by waves 0 .. MF - 1, weight fragments
+    // (lane f: fragment f) by wave MF, a placeholder by the others
+    if (wi < MF) {
+      sb = reinterpret_cast<const uint8_t *>(uni_ptr(q->a_scales));
+      os = src(rt, 64 * wi + ln) * 4u;
     } else {
-      float m = 0.0f;
+      sb = reinterpret_cast<const uint8_t *>(uni_ptr(q->w_scales + (int64_t)itl.e * NB * KB));
+      const int f = ln & 7;
+      os = wi == MF ? (uint32_t)(bk_wrow<GLU>(32 * f, itl.nt, N) / FB) * (uint32_t)KB * 4u : 0u;
+    }
+    left = nst;
+    if (it + nsl < t_end) {
+      nx = pn_locate<MF>(S, it + nsl, ecur, lane);
+      tok_dma(nx, ibuf ^ 1);
+    }
+  };
+  // a stage of loads into the slot at LDS address at, LPS per wave always
+  // (placeholders past the last tile), so that the waits can count
+  auto loads = [&](uint32_t at) __attribute__((always_inline)) {
+    const int kb = nst - 1 - left;             // left has been counted down
+    if ((kb + 1) * FB <= K) {
 #pragma unroll
-      for (int q = 0; q < 16; ++q)
-        if (col0[0] < I) m = fmaxf(m, fabsf(v[q]));
-      m = fmaxf(m, __shfl_xor(m, 32, 64));
-      if (h == 0) sh_m[w][c] = m;
-      __syncthreads();
-      m = fmaxf(fmaxf(sh_m[0][c], sh_m[1][c]), fmaxf(sh_m[2][c], sh_m[3][c]));
-      float enc, dec;
-      fb_scale(m, enc, dec);
-      if (in_row && w == 0 && h == 0) p.out_scales[(int64_t)tl.nt * p.rows + row] = dec;
+      for (int j = 0; j < MF; ++j) dma16s(pa, oa[j], uni(at + (w + 8 * j) * 1024));
 #pragma unroll
-      for (int q = 0; q < 16; q += 4) {
-        const int n = col0[0] + 2 * q + 4 * h;
-        if (in_row && n < I)
-          *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(p.out) + row * I + n) =
-              fb_codes4(v[q], v[q + 1], v[q + 2], v[q + 3], enc);
+      for (int j = 0; j < 4; ++j) dma16s(wb, ob[j], uni(at + C::BOFF + (w + 8 * j) * 1024));
+    } else {                                   // the last block is short: zeros past K
+      const bool in = kb * FB + (int)pc < K;
+      const uint8_t *z = reinterpret_cast<const uint8_t *>(&bk_zero);
+#pragma unroll
+      for (int j = 0; j < MF; ++j) dma16(in ? pa + oa[j] : z, uni(at + (w + 8 * j) * 1024));
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        dma16(in ? wb + ob[j] : z, uni(at + C::BOFF + (w + 8 * j) * 1024));
+    }
+    dma4s(sb, os, uni(w <= MF ? at + C::SOFF + w * 256 : dummy));
+    pa += FB;
+    wb += FB;
+    if (kb + 1 < KB) sb += w < MF ? bk_args()->a_rows * 4 : w == MF ? 4 : 0;
+  };
+  auto issue = [&](uint32_t at) __attribute__((always_inline)) {
+    if (left == 0) {
+      it += nsl;
+      if (it < t_end) {
+        itl = nx;
+        ibuf ^= 1;
+        bind();
+      } else {
+        left = 0x7fffffff;
       }
     }
+    --left;
+    if (it < t_end) {
+      loads(at);
+    } else {
+      const uint8_t *any = uni_ptr(bk_args()->a);
+#pragma unroll
+      for (int j = 0; j < C::LPS; ++j) dma4s(any, 0u, uni(dummy));
+    }
+  };
+
+  if (it < t_end) {
+    itl = pn_locate<MF>(S, it, ecur, lane);
+    tok_dma(itl, 0);
+    wait_vm<0>();
+    pn_barrier();
+    bind();
+    for (int q = 0; q < ns; ++q) {         // ns <= nst: stages of this tile
+      --left;
+      loads(uni(lds0 + q * C::SLOT));
+    }
+    pn_wait<C::LPS>(ns - 1);
+    pn_barrier();
   }
+  int slot = 0;
+  PnTile cur = itl;
+  while (ct < t_end) {
+    const int nt = cur.nt, row0 = cur.row0, nrows = cur.nrows;
+    const int nfr = (nrows + 31) >> 5, half = (nfr + 1) >> 1;
+    const int fa0 = wm ? half : 0;
+    const int mtv = wm ? nfr - half : half;
+    const int fb0 = GLU ? wn : 2 * wn;
+    constexpr int FBS = GLU ? 4 : 1;       // the wave's second fragment: fb0 + FBS
+
+    auto run = [&](auto mtv_c) __attribute__((always_inline)) {
+      constexpr int MTV = decltype(mtv_c)::value;
+      constexpr int MA = MTV > 0 ? MTV : 1;
+      constexpr int ITEMS = 2 * MA;            // (half of the block, row fragment)
+      f32x16 acc[MA][2], part[MA][2];
+      float sc[MA][2];
+#pragma unroll
+      for (int i = 0; i < MA; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          sc[i][j] = 0.0f;
+#pragma unroll
+          for (int q = 0; q < 16; ++q) acc[i][j][q] = part[i][j][q] = 0.0f;
+        }
+      const int r = lane & 31, h = lane >> 5, sw = bk_swz(r);
+      struct Op {
+        uint4 c[2];
+      };
+      const int la = (32 * fa0 + r) * 128;
+      // half st of row fragment i, of weight fragment f
+      auto rd_a = [&](const unsigned char *sl, int n) __attribute__((always_inline)) -> Op {
+        Op o;
+        const int st = n / MA, i = n % MA;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          o.c[k] = *reinterpret_cast<const uint4 *>(sl + la + i * 4096 +
+                                                    (((4 * st + 2 * h + k) ^ sw) << 4));
+        return o;
+      };
+      auto rd_b = [&](const unsigned char *sl, int st, int j) __attribute__((always_inline)) -> Op {
+        Op o;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          o.c[k] = *reinterpret_cast<const uint4 *>(
+              sl + C::BOFF + (32 * (fb0 + j * FBS) + r) * 128 + (((4 * st + 2 * h + k) ^ sw) << 4));
+        return o;
+      };
+      auto step8 = [](const Op &o, int ks) __attribute__((always_inline)) -> f16x8 {
+        const uint4 q = o.c[ks >> 1];
+        return (ks & 1) ? dec8(q.z, q.w) : dec8(q.x, q.y);
+      };
+      auto sync = [&]() __attribute__((always_inline)) -> uint32_t {
+        pn_wait<C::LPS>(ns - 2);
+        pn_barrier();
+        const uint32_t at = uni(lds0 + slot * C::SLOT);
+        slot = slot + 1 == ns ? 0 : slot + 1;
+        return at;
+      };
+      auto fold = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            acc[i][j][q] = __builtin_fmaf(part[i][j][q], sc[i][j], acc[i][j][q]);
+      };
+      for (int s = 0; s < nst; ++s) {
+        if constexpr (MTV == 0) {
+          issue(sync());
+        } else {
+          const unsigned char *sl = lds + slot * C::SLOT;
+          const float *ss = reinterpret_cast<const float *>(sl + C::SOFF);
+          const float w0 = ss[64 * MF + fb0], w1 = ss[64 * MF + fb0 + FBS];
+          f16x8 b[2][4];
+          Op a = rd_a(sl, 0);
+#pragma unroll
+          for (int n = 0; n < ITEMS; ++n) {
+            const int st = n / MA, i = n % MA;
+            if (i == 0) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const Op o = rd_b(sl, st, j);
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) b[j][ks] = step8(o, ks);
+              }
+            }
+            Op an = a;
+            if (n + 1 < ITEMS) an = rd_a(sl, n + 1);
+            if (st == 0) {
+              fold(i);
+              const float ra = ss[32 * (fa0 + i) + r];
+              sc[i][0] = ra * w0;
+              sc[i][1] = ra * w1;
+            }
+            f32x16 z;
+#pragma unroll
+            for (int q = 0; q < 16; ++q) z[q] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+              const f16x8 av = step8(a, ks);
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                part[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                    b[j][ks], av, st == 0 && ks == 0 ? z : part[i][j], 0, 0, 0);
+            }
+            a = an;
+          }
+          issue(sync());
+        }
+      }
+      if constexpr (MTV > 0) {
+#pragma unroll
+        for (int i = 0; i < MA; ++i) fold(i);
+      }
+      // ---- epilogue.  Element q of a fragment: column 8 (q / 4) + 4 h + q % 4 of row r
+      const int ldo = pn_fresh_s(GLU ? N >> 1 : N);
+      const int ln = pn_fresh(lane), rr = ln & 31, hh = ln >> 5;
+      if constexpr (MTV > 0) {
+        if constexpr (GLU) {
+#pragma unroll
+          for (int i = 0; i < MA; ++i)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[i][0][q] = bk_swiglu(acc[i][0][q], acc[i][1][q]);
+        }
+      }
+      if constexpr (EPI == QD_EPI_SWIGLU_FP8) {
+        // the maximum over the four waves' columns, each 32 of the block
+        const int cb0 = nt * 128 + 32 * wn;
+        if constexpr (MTV > 0) {
+#pragma unroll
+          for (int i = 0; i < MA; ++i) {
+            float m = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 16; ++q) m = fmaxf(m, fabsf(acc[i][0][q]));
+            m = cb0 < ldo ? fmaxf(m, __shfl_xor(m, 32, 64)) : 0.0f;
+            if (hh == 0) amax[wn * C::M + 32 * (fa0 + i) + rr] = m;
+          }
+        }
+        pn_barrier();
+        if constexpr (MTV > 0) {
+#pragma unroll
+          for (int i = 0; i < MA; ++i) {
+            const int rl = 32 * (fa0 + i) + rr;
+            const float m = fmaxf(fmaxf(amax[rl], amax[C::M + rl]),
+                                  fmaxf(amax[2 * C::M + rl], amax[3 * C::M + rl]));
+            float enc, dec;
+            fb_scale(m, enc, dec);
+            uint32_t cq[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              cq[q] = fb_codes4(acc[i][0][4 * q], acc[i][0][4 * q + 1], acc[i][0][4 * q + 2],
+                                acc[i][0][4 * q + 3], enc);
+            const Pair32 u = swap32(cq[0], cq[2]), v = swap32(cq[1], cq[3]);
+            const bool in = rl < nrows && cb0 < ldo;
+            const BkArgPtr g = bk_args();
+            if (in)
+              *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(g->out) +
+                                         (int64_t)(row0 + rl) * ldo + cb0 + 16 * hh) =
+                  make_uint4(u.x, u.y, v.x, v.y);
+            if (in && wn == 0 && hh == 0) g->out_scales[(int64_t)nt * g->rows + row0 + rl] = dec;
+          }
+        }
+      } else if constexpr (MTV > 0) {
+        constexpr int NO = GLU ? 1 : 2;
+#pragma unroll
+        for (int i = 0; i < MA; ++i)
+#pragma unroll
+          for (int j = 0; j < NO; ++j) {
+            const int cb0 = GLU ? nt * 128 + 32 * wn : nt * PN_N + 32 * (fb0 + j);
+            const int rl = 32 * (fa0 + i) + rr;
+            uint32_t bq[4][2];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int k = 0; k < 2; ++k)
+                bq[q][k] = bf16_pair(acc[i][j][4 * q + 2 * k], acc[i][j][4 * q + 2 * k + 1]);
+            uint16_t *o = static_cast<uint16_t *>(bk_args()->out) + (int64_t)(row0 + rl) * ldo +
+                          cb0 + 16 * hh;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              const Pair32 u = swap32(bq[q][0], bq[q + 2][0]), v = swap32(bq[q][1], bq[q + 2][1]);
+              if (rl < nrows && cb0 + 16 * hh + 8 * q < ldo)
+                *reinterpret_cast<uint4 *>(o + 8 * q) = make_uint4(u.x, v.x, u.y, v.y);
+            }
+          }
+      }
+      // the stores' lane branches join here, so that they do not make the
+      // scalar state of the tile loop look divergent to the compiler
+      asm volatile("" ::: "memory");
+    };
+    auto pick = [&](auto self, auto n_c) __attribute__((always_inline)) {
+      constexpr int n = decltype(n_c)::value;
+      if constexpr (n == 0) {
+        run(std::integral_constant<int, 0>{});
+      } else {
+        if (mtv == n) run(std::integral_constant<int, n>{});
+        else self(self, std::integral_constant<int, n - 1>{});
+      }
+    };
+    pick(pick, std::integral_constant<int, MF>{});
+    // the issue cursor is ns (<= nst) stages ahead: at the next tile
+    ct += nsl;
+    cur = itl;
+  }
+  wait_vm<0>();
+}
+
+constexpr double BK_TILE = 2.0;        // a tile's fixed time, in that of a 32-row fragment
+
+struct BlkPlan {
+  int mf, ns, grid, lds;
+  PnDeal deal;
+};
+
+inline BlkPlan blk_plan(int64_t rows, int E, int64_t N, int64_t K, int epilogue) {
+  BlkPlan pl{};
+  const int nst = std::max(2, (int)((K + FB - 1) / FB));
+  const int ntn = (int)((N + PN_N - 1) / PN_N);
+  const PnHeight h = pn_height(rows, E, ntn, BK_TILE, true, false, [&](int mf) {
+    if (mf > 2) return 0;
+    int ns = std::min(5, nst);
+    while (ns >= 2 && bk_layout(mf, ns, E).total > PN_LDS_MAX) --ns;
+    return ns;
+  });
+  pl.mf = h.mf;
+  pl.ns = h.ns;
+  pl.lds = bk_layout(h.mf, h.ns, E).total;
+  pl.grid = (int)std::min<int64_t>(256, qdt::tile_grid(rows, E, 64 * pl.mf, ntn));
+  pl.deal = pn_deal(h, ntn, pl.grid);
+  return pl;
+}
+
+template <int MF, int EPI>
+void launch_blk_one(const BlkArgs &p, const BlkPlan &pl, hipStream_t s) {
+  auto kern = gemm_block_kernel<MF, EPI>;
+  static const bool attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize,
+                                               PN_LDS_MAX) == hipSuccess;
+  (void)attr;
+  hipLaunchKernelGGL(kern, dim3((unsigned)pl.grid), dim3(PN_THREADS), (size_t)pl.lds, s, p, pl.deal,
+                     pl.ns);
+}
+template <int EPI>
+void launch_blk(const BlkArgs &p, const BlkPlan &pl, hipStream_t s) {
+  if (pl.mf == 2) launch_blk_one<2, EPI>(p, pl, s);
+  else launch_blk_one<1, EPI>(p, pl, s);
 }
 
 }  // namespace
@@ -178,23 +532,17 @@ extern "C" qd_status moe_fp8_block_grouped_gemm(
       ((uintptr_t)row_token & 3u) || ((uintptr_t)expert_offsets & 3u))
     return QD_ERR_ALIGN;
   const int64_t lim = 1LL << 32;
-  if (E > BK_EMAX || rows > 0x7fffffffLL || a_rows > 0x7fffffffLL || N > 0x3fffffffLL ||
+  if (E > PN_EMAX || rows > 0x7fffffffLL || a_rows > 0x7fffffffLL || N > 0x3fffffffLL ||
       K > 0x3fffffffLL || (a_rows > rows ? a_rows : rows) + 1 > lim / K || N > (lim - 1) / K)
     return QD_ERR_UNSUPPORTED;
   if (qdh::fault_injected()) return QD_ERR_HIP;
   if (rows == 0) return QD_OK;
   BlkArgs p{a_codes, a_scales, a_rows, row_token, expert_offsets, E, rows, w_codes, w_scales,
             (int)N, (int)K, out, out_scales};
-  const int ntn = (int)((N + 255) / 256);
-  const int64_t g = qdt::tile_grid(rows, E, 32, ntn);
-  if (g > 0x7fffffffLL) return QD_ERR_UNSUPPORTED;
+  const BlkPlan pl = blk_plan(rows, E, N, K, epilogue);
   hipStream_t s = qdh::S(stream);
-  const dim3 grid((unsigned)g), block(256);
-  if (epilogue == QD_EPI_NONE)
-    hipLaunchKernelGGL(gemm_block_kernel<QD_EPI_NONE>, grid, block, 0, s, p, ntn);
-  else if (epilogue == QD_EPI_SWIGLU)
-    hipLaunchKernelGGL(gemm_block_kernel<QD_EPI_SWIGLU>, grid, block, 0, s, p, ntn);
-  else
-    hipLaunchKernelGGL(gemm_block_kernel<QD_EPI_SWIGLU_FP8>, grid, block, 0, s, p, ntn);
+  if (epilogue == QD_EPI_NONE) launch_blk<QD_EPI_NONE>(p, pl, s);
+  else if (epilogue == QD_EPI_SWIGLU) launch_blk<QD_EPI_SWIGLU>(p, pl, s);
+  else launch_blk<QD_EPI_SWIGLU_FP8>(p, pl, s);
   return qdh::check_launch();
 }
