@@ -15,10 +15,13 @@
 // register, the weight scale is uniform, and the columns of a row leave a lane together.
 //
 //  * Workgroup tile: up to 64 MF rows of one expert x 256 weight rows (SwiGLU: 128 gate
-//    rows and the matching up rows, one block of 128 of h), eight waves in a 2 x 4 grid of
-//    32 MF rows x 64 weight rows.  The schedule is the NVFP4 panel kernel's
-//    (panel_sched.h): one persistent workgroup per CU, its tiles' stages one stream
-//    through an LDS ring filled by direct global->LDS loads.
+//    rows and the matching up rows, one block of 128 of h; a fragment of 32 holds 16 of
+//    each, so that a lane has both), eight waves in a 2 x 4 grid.  A wave has two weight
+//    fragments and half of the tile's row fragments; of an odd last one each half of the
+//    grid takes one weight fragment, so that a tile of n row fragments costs n / 2 of
+//    them whatever n is.  The schedule is the NVFP4 panel kernel's (panel_sched.h): one
+//    persistent workgroup per CU, its tiles' stages one stream through an LDS ring
+//    filled by direct global->LDS loads.
 //  * A stage is one block of K: 128 bytes of every row, the tile's row scales of that
 //    block and the scales of its weight fragments.  Pieces of 16 bytes past K come from a
 //    zero in memory.  The pieces of a row are placed by a row-dependent XOR, so the
@@ -89,17 +92,19 @@ struct BkCfg {
   static constexpr int LPS = MF + 4 + 1;               // loads per wave and stage
 };
 
+constexpr int BK_NS = 3;             // stages of the ring
+
 struct BkLayout {
   int tok, amax, dummy, offs, mpre, perm, total;
 };
 // after the ring: the tokens of two tiles, the waves' row maxima (quantising
 // epilogue), the target of placeholder loads, the tile schedule
-__host__ __device__ inline BkLayout bk_layout(int mf, int ns, int E) {
+__host__ __device__ inline BkLayout bk_layout(int mf, int E) {
   BkLayout L{};
-  int o = ns * (64 * mf * 128 + 32768 + (mf + 1) * 256);
+  int o = BK_NS * (64 * mf * 128 + 32768 + (mf + 1) * 256);
   auto take = [&](int bytes) { const int at = o; o += (bytes + 15) & ~15; return at; };
   L.tok = take(2 * 64 * mf * 4);
-  L.amax = take(4 * 64 * mf * 4);
+  L.amax = take(8 * 64 * mf * 4);
   L.dummy = take(256);
   L.offs = take((E + 1) * 4);
   L.mpre = take((E + 1) * 4);
@@ -118,19 +123,20 @@ __device__ __forceinline__ BkArgPtr bk_args() {
 // 16-byte piece c of tile row r sits at piece c ^ bk_swz(r) of the row's 128
 __device__ __forceinline__ int bk_swz(int r) { return (r >> 1) & 7; }
 
-// weight row of the tile's row tb (0 past the last: never stored)
+// weight row of the tile's row tb (0 past the last: never stored); SwiGLU: a fragment of
+// 32 is 16 gate rows and the 16 up rows of the same columns
 template <bool GLU>
 __device__ __forceinline__ int bk_wrow(int tb, int nt, int N) {
   if (GLU) {
-    const int I = N >> 1, c = nt * 128 + (tb & 127);
-    return c < I ? c + (tb < 128 ? 0 : I) : 0;
+    const int I = N >> 1, c = nt * 128 + 16 * (tb >> 5) + (tb & 15);
+    return c < I ? c + (tb & 16 ? I : 0) : 0;
   }
   const int c = nt * PN_N + tb;
   return c < N ? c : 0;
 }
 
 template <int MF, int EPI>
-__global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, PnDeal deal, int ns) {
+__global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, PnDeal deal) {
   using C = BkCfg<MF>;
   constexpr bool GLU = EPI != QD_EPI_NONE;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -139,8 +145,8 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   const int tid = threadIdx.x, lane = tid & 63, w = (int)uni((uint32_t)tid >> 6);
   const int N = p.N, E = p.E, K = p.K;
   const int KB = (K + FB - 1) / FB, NB = (N + FB - 1) / FB;
-  const int nst = KB > 2 ? KB : 2;             // two stages at least (zeros past K)
-  const BkLayout L = bk_layout(MF, ns, E);
+  const int nst = KB > BK_NS ? KB : BK_NS;     // a whole ring at least (zeros past K)
+  const BkLayout L = bk_layout(MF, E);
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   int32_t *offs = reinterpret_cast<int32_t *>(lds + L.offs);
   int32_t *mpre = reinterpret_cast<int32_t *>(lds + L.mpre);
@@ -191,15 +197,14 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       ob[j] = (uint32_t)bk_wrow<GLU>(8 * (wi + 8 * j) + (ln >> 3), itl.nt, N) * (uint32_t)K + pc;
-    // the stage's scales: rows of the tile by waves 0 .. MF - 1, weight fragments
-    // (lane f: fragment f) by wave MF, a placeholder by the others
+    // the stage's scales: rows of the tile by waves 0 .. MF - 1, weights (lane f: the
+    // tile's rows from 16 f on) by wave MF, a placeholder by the others
     if (wi < MF) {
       sb = reinterpret_cast<const uint8_t *>(uni_ptr(q->a_scales));
       os = src(rt, 64 * wi + ln) * 4u;
     } else {
       sb = reinterpret_cast<const uint8_t *>(uni_ptr(q->w_scales + (int64_t)itl.e * NB * KB));
-      const int f = ln & 7;
-      os = wi == MF ? (uint32_t)(bk_wrow<GLU>(32 * f, itl.nt, N) / FB) * (uint32_t)KB * 4u : 0u;
+      os = wi == MF ? (uint32_t)(bk_wrow<GLU>(16 * (ln & 15), itl.nt, N) / FB) * (uint32_t)KB * 4u : 0u;
     }
     left = nst;
     if (it + nsl < t_end) {
@@ -257,49 +262,48 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
     wait_vm<0>();
     pn_barrier();
     bind();
-    for (int q = 0; q < ns; ++q) {         // ns <= nst: stages of this tile
+    for (int q = 0; q < BK_NS; ++q) {      // stages of this tile
       --left;
       loads(uni(lds0 + q * C::SLOT));
     }
-    pn_wait<C::LPS>(ns - 1);
+    wait_vm<(BK_NS - 1) * C::LPS>();
     pn_barrier();
   }
   int slot = 0;
   PnTile cur = itl;
   while (ct < t_end) {
     const int nt = cur.nt, row0 = cur.row0, nrows = cur.nrows;
-    const int nfr = (nrows + 31) >> 5, half = (nfr + 1) >> 1;
-    const int fa0 = wm ? half : 0;
-    const int mtv = wm ? nfr - half : half;
-    const int fb0 = GLU ? wn : 2 * wn;
-    constexpr int FBS = GLU ? 4 : 1;       // the wave's second fragment: fb0 + FBS
+    const int nfr = (nrows + 31) >> 5;
 
-    auto run = [&](auto mtv_c) __attribute__((always_inline)) {
-      constexpr int MTV = decltype(mtv_c)::value;
-      constexpr int MA = MTV > 0 ? MTV : 1;
+    // FULL row fragments of this wave's half with both weight fragments, and HALF: the
+    // tile's last one with the first of them
+    auto run = [&](auto nfr_c) __attribute__((always_inline)) {
+      constexpr int FULL = decltype(nfr_c)::value / 2, HALF = decltype(nfr_c)::value % 2;
+      constexpr int MA = FULL + HALF, NJ = FULL > 0 ? 2 : 1;
       constexpr int ITEMS = 2 * MA;            // (half of the block, row fragment)
+      constexpr int NS = GLU ? 2 : 1;          // scales of a fragment: gate and up halves
       f32x16 acc[MA][2], part[MA][2];
-      float sc[MA][2];
+      auto nj = [](int i) { return i < FULL ? 2 : 1; };
 #pragma unroll
       for (int i = 0; i < MA; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          sc[i][j] = 0.0f;
+        for (int j = 0; j < nj(i); ++j)
 #pragma unroll
           for (int q = 0; q < 16; ++q) acc[i][j][q] = part[i][j][q] = 0.0f;
-        }
       const int r = lane & 31, h = lane >> 5, sw = bk_swz(r);
       struct Op {
         uint4 c[2];
       };
-      const int la = (32 * fa0 + r) * 128;
-      // half st of row fragment i, of weight fragment f
+      // row fragment i, weight fragment j (the grid's halves take them in either order)
+      auto fa = [&](int i) __attribute__((always_inline)) { return i < FULL ? wm * FULL + i : 2 * FULL; };
+      auto fb = [&](int j) __attribute__((always_inline)) { return 2 * wn + (j ^ wm); };
+      // half st of row fragment i, of weight fragment j
       auto rd_a = [&](const unsigned char *sl, int n) __attribute__((always_inline)) -> Op {
         Op o;
         const int st = n / MA, i = n % MA;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          o.c[k] = *reinterpret_cast<const uint4 *>(sl + la + i * 4096 +
+          o.c[k] = *reinterpret_cast<const uint4 *>(sl + (32 * fa(i) + r) * 128 +
                                                     (((4 * st + 2 * h + k) ^ sw) << 4));
         return o;
       };
@@ -307,8 +311,8 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
         Op o;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          o.c[k] = *reinterpret_cast<const uint4 *>(
-              sl + C::BOFF + (32 * (fb0 + j * FBS) + r) * 128 + (((4 * st + 2 * h + k) ^ sw) << 4));
+          o.c[k] = *reinterpret_cast<const uint4 *>(sl + C::BOFF + (32 * fb(j) + r) * 128 +
+                                                    (((4 * st + 2 * h + k) ^ sw) << 4));
         return o;
       };
       auto step8 = [](const Op &o, int ks) __attribute__((always_inline)) -> f16x8 {
@@ -316,136 +320,199 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
         return (ks & 1) ? dec8(q.z, q.w) : dec8(q.x, q.y);
       };
       auto sync = [&]() __attribute__((always_inline)) -> uint32_t {
-        pn_wait<C::LPS>(ns - 2);
+        wait_vm<(BK_NS - 2) * C::LPS>();
         pn_barrier();
         const uint32_t at = uni(lds0 + slot * C::SLOT);
-        slot = slot + 1 == ns ? 0 : slot + 1;
+        slot = slot + 1 == BK_NS ? 0 : slot + 1;
         return at;
       };
-      auto fold = [&](int i) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int q = 0; q < 16; ++q)
-            acc[i][j][q] = __builtin_fmaf(part[i][j][q], sc[i][j], acc[i][j][q]);
+      struct Scales {
+        float w[NS], r[MA];
       };
+      auto rd_s = [&](const unsigned char *sl) __attribute__((always_inline)) -> Scales {
+        const float *ss = reinterpret_cast<const float *>(sl + C::SOFF);
+        Scales o;
+#pragma unroll
+        for (int g = 0; g < NS; ++g) o.w[g] = ss[64 * MF + 4 * wn + g];
+#pragma unroll
+        for (int i = 0; i < MA; ++i) o.r[i] = ss[32 * fa(i) + r];
+        return o;
+      };
+      // quarter ks of a row fragment's partial sums into its totals
+      auto fold = [&](int i, int ks, const Scales &v) __attribute__((always_inline)) {
+        float sc[NS];
+#pragma unroll
+        for (int g = 0; g < NS; ++g) sc[g] = v.r[i] * v.w[g];
+        const int n = 4 * nj(i);
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+          const int j = (ks * n + e) >> 4, q = (ks * n + e) & 15;
+          acc[i][j][q] = __builtin_fmaf(part[i][j][q], sc[GLU ? q >> 3 : 0], acc[i][j][q]);
+        }
+        // here and not where the compiler would sink it, past the loop's branches
+#pragma unroll
+        for (int j = 0; j < nj(i); ++j)
+          if (j == (ks * n) >> 4 || j == (ks * n + n - 1) >> 4) asm volatile("" : "+v"(acc[i][j]));
+      };
+      // The stream of one wave: per k-step of 16 the MFMAs of its operands, beside them
+      // the decoding of the next step's and a quarter of a fold, held together by the
+      // scheduling barriers.  (Both waves of a SIMD run in step: VALU work in lumps
+      // leaves the matrix unit idle for both.)  Codes are read an item ahead; the
+      // workgroup's barrier stands before the last item, whose codes are in registers.
+      // The partial sums of fragment i are folded just before they start anew.
+      Op bq[NJ];
+      const unsigned char *s0 = lds + slot * C::SLOT;
+      Op a = rd_a(s0, 0);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) bq[j] = rd_b(s0, 0, j);
+      Scales sv = rd_s(s0), sp;
+#pragma unroll
+      for (int g = 0; g < NS; ++g) sp.w[g] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < MA; ++i) sp.r[i] = 0.0f;
+      f16x8 av = step8(a, 0), b[NJ][4];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) b[j][0] = step8(bq[j], 0);
       for (int s = 0; s < nst; ++s) {
-        if constexpr (MTV == 0) {
-          issue(sync());
-        } else {
-          const unsigned char *sl = lds + slot * C::SLOT;
-          const float *ss = reinterpret_cast<const float *>(sl + C::SOFF);
-          const float w0 = ss[64 * MF + fb0], w1 = ss[64 * MF + fb0 + FBS];
-          f16x8 b[2][4];
-          Op a = rd_a(sl, 0);
+        const unsigned char *sl = lds + slot * C::SLOT;
+        Scales sn;
 #pragma unroll
-          for (int n = 0; n < ITEMS; ++n) {
-            const int st = n / MA, i = n % MA;
-            if (i == 0) {
+        for (int n = 0; n < ITEMS; ++n) {
+          const int st = n / MA, i = n % MA;
+          const bool last = n + 1 == ITEMS, turn = i == MA - 1;   // turn: the next item is fragment 0
+          Op an, bn[NJ];
+          uint32_t at = 0;
+          if (last) {
+            at = sync();
+            sl = lds + slot * C::SLOT;         // (past the last stage: the next tile's, unused)
+            sn = rd_s(sl);
+          }
+          an = rd_a(sl, last ? 0 : n + 1);
+          if (turn) {
 #pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const Op o = rd_b(sl, st, j);
+            for (int j = 0; j < NJ; ++j) bn[j] = rd_b(sl, last ? 0 : 1, j);
+          }
+          if (MA == 1 && st == 0) {
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks) b[j][ks] = step8(o, ks);
-              }
-            }
-            Op an = a;
-            if (n + 1 < ITEMS) an = rd_a(sl, n + 1);
-            if (st == 0) {
-              fold(i);
-              const float ra = ss[32 * (fa0 + i) + r];
-              sc[i][0] = ra * w0;
-              sc[i][1] = ra * w1;
-            }
+            for (int ks = 0; ks < 4; ++ks) fold(0, ks, sp);
+          }
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks) {
+            __builtin_amdgcn_sched_barrier(0);
             f32x16 z;
 #pragma unroll
             for (int q = 0; q < 16; ++q) z[q] = 0.0f;
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-              const f16x8 av = step8(a, ks);
+            for (int j = 0; j < nj(i); ++j)
+              part[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                  b[j][ks], av, st == 0 && ks == 0 ? z : part[i][j], 0, 0, 0);
+            if (ks < 3) {
+              av = step8(a, ks + 1);
+              if (i == 0) {
 #pragma unroll
-              for (int j = 0; j < 2; ++j)
-                part[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                    b[j][ks], av, st == 0 && ks == 0 ? z : part[i][j], 0, 0, 0);
+                for (int j = 0; j < NJ; ++j) b[j][ks + 1] = step8(bq[j], ks + 1);
+              }
+            } else {
+              av = step8(an, 0);
+              if (turn) {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) b[j][0] = step8(bn[j], 0);
+              }
             }
-            a = an;
+            if (MA > 1 && last) fold(0, ks, sv);
+            if (st == 0 && !turn) fold(i + 1, ks, sp);
           }
-          issue(sync());
-        }
-      }
-      if constexpr (MTV > 0) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (last) issue(at);
+          a = an;
+          if (turn) {
 #pragma unroll
-        for (int i = 0; i < MA; ++i) fold(i);
+            for (int j = 0; j < NJ; ++j) bq[j] = bn[j];
+          }
+        }
+        sp = sv;
+        sv = sn;
       }
-      // ---- epilogue.  Element q of a fragment: column 8 (q / 4) + 4 h + q % 4 of row r
+#pragma unroll
+      for (int i = MA > 1 ? 1 : 0; i < MA; ++i)
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) fold(i, ks, sp);
+      // ---- epilogue.  Element q of a fragment: its weight row 8 (q / 4) + 4 h + q % 4, row r
+      // of the rows; with SwiGLU q and q + 8 are gate and up of column 8 (q / 4) + 4 h + q % 4
+      // of 16.  Four consecutive columns are a quad; the halves of the wave swap quads, so that
+      // a lane stores 8 or 16 consecutive columns.
       const int ldo = pn_fresh_s(GLU ? N >> 1 : N);
       const int ln = pn_fresh(lane), rr = ln & 31, hh = ln >> 5;
-      if constexpr (MTV > 0) {
-        if constexpr (GLU) {
-#pragma unroll
-          for (int i = 0; i < MA; ++i)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) acc[i][0][q] = bk_swiglu(acc[i][0][q], acc[i][1][q]);
-        }
-      }
-      if constexpr (EPI == QD_EPI_SWIGLU_FP8) {
-        // the maximum over the four waves' columns, each 32 of the block
-        const int cb0 = nt * 128 + 32 * wn;
-        if constexpr (MTV > 0) {
-#pragma unroll
-          for (int i = 0; i < MA; ++i) {
-            float m = 0.0f;
-#pragma unroll
-            for (int q = 0; q < 16; ++q) m = fmaxf(m, fabsf(acc[i][0][q]));
-            m = cb0 < ldo ? fmaxf(m, __shfl_xor(m, 32, 64)) : 0.0f;
-            if (hh == 0) amax[wn * C::M + 32 * (fa0 + i) + rr] = m;
-          }
-        }
-        pn_barrier();
-        if constexpr (MTV > 0) {
-#pragma unroll
-          for (int i = 0; i < MA; ++i) {
-            const int rl = 32 * (fa0 + i) + rr;
-            const float m = fmaxf(fmaxf(amax[rl], amax[C::M + rl]),
-                                  fmaxf(amax[2 * C::M + rl], amax[3 * C::M + rl]));
-            float enc, dec;
-            fb_scale(m, enc, dec);
-            uint32_t cq[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              cq[q] = fb_codes4(acc[i][0][4 * q], acc[i][0][4 * q + 1], acc[i][0][4 * q + 2],
-                                acc[i][0][4 * q + 3], enc);
-            const Pair32 u = swap32(cq[0], cq[2]), v = swap32(cq[1], cq[3]);
-            const bool in = rl < nrows && cb0 < ldo;
-            const BkArgPtr g = bk_args();
-            if (in)
-              *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(g->out) +
-                                         (int64_t)(row0 + rl) * ldo + cb0 + 16 * hh) =
-                  make_uint4(u.x, u.y, v.x, v.y);
-            if (in && wn == 0 && hh == 0) g->out_scales[(int64_t)nt * g->rows + row0 + rl] = dec;
-          }
-        }
-      } else if constexpr (MTV > 0) {
-        constexpr int NO = GLU ? 1 : 2;
+      if constexpr (GLU) {
 #pragma unroll
         for (int i = 0; i < MA; ++i)
 #pragma unroll
-          for (int j = 0; j < NO; ++j) {
-            const int cb0 = GLU ? nt * 128 + 32 * wn : nt * PN_N + 32 * (fb0 + j);
-            const int rl = 32 * (fa0 + i) + rr;
-            uint32_t bq[4][2];
+          for (int j = 0; j < nj(i); ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 8; ++q)
+              acc[i][j][q] = bk_swiglu(acc[i][j][q], acc[i][j][q + 8]);
+      }
+      // first column of fragment j
+      auto col = [&](int j) __attribute__((always_inline)) {
+        return GLU ? nt * 128 + 16 * fb(j) : nt * PN_N + 32 * fb(j);
+      };
+      if constexpr (EPI == QD_EPI_SWIGLU_FP8) {
+        // the maximum over the block's columns, 16 of each fragment
 #pragma unroll
-              for (int k = 0; k < 2; ++k)
-                bq[q][k] = bf16_pair(acc[i][j][4 * q + 2 * k], acc[i][j][4 * q + 2 * k + 1]);
-            uint16_t *o = static_cast<uint16_t *>(bk_args()->out) + (int64_t)(row0 + rl) * ldo +
-                          cb0 + 16 * hh;
+        for (int i = 0; i < MA; ++i) {
+          float m = 0.0f;
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              const Pair32 u = swap32(bq[q][0], bq[q + 2][0]), v = swap32(bq[q][1], bq[q + 2][1]);
-              if (rl < nrows && cb0 + 16 * hh + 8 * q < ldo)
-                *reinterpret_cast<uint4 *>(o + 8 * q) = make_uint4(u.x, v.x, u.y, v.y);
+          for (int j = 0; j < nj(i); ++j)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) m = fmaxf(m, fabsf(acc[i][j][q]));
+          m = col(0) < ldo ? fmaxf(m, __shfl_xor(m, 32, 64)) : 0.0f;
+          if (hh == 0) amax[(i < FULL ? wn : wn + 4 * wm) * C::M + 32 * fa(i) + rr] = m;
+        }
+        pn_barrier();
+#pragma unroll
+        for (int i = 0; i < MA; ++i) {
+          const int rl = 32 * fa(i) + rr;
+          float m = 0.0f;
+#pragma unroll
+          for (int k = 0; k < (i < FULL ? 4 : 8); ++k) m = fmaxf(m, amax[k * C::M + rl]);
+          float enc, dec;
+          fb_scale(m, enc, dec);
+          const BkArgPtr g = bk_args();
+          const bool in = rl < nrows;
+          uint8_t *o = static_cast<uint8_t *>(g->out) + (int64_t)(row0 + rl) * ldo;
+#pragma unroll
+          for (int j = 0; j < nj(i); ++j) {
+            const uint32_t q0 = fb_codes4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], enc);
+            const uint32_t q1 = fb_codes4(acc[i][j][4], acc[i][j][5], acc[i][j][6], acc[i][j][7], enc);
+            const Pair32 u = swap32(q0, q1);
+            if (in && col(j) < ldo)
+              *reinterpret_cast<uint2 *>(o + col(j) + 8 * hh) = make_uint2(u.x, u.y);
+          }
+          if (in && hh == 0 && (i < FULL ? wn : w) == 0)
+            g->out_scales[(int64_t)nt * g->rows + row0 + rl] = dec;
+        }
+      } else {
+        constexpr int QP = GLU ? 1 : 2;        // pairs of quads of a fragment
+#pragma unroll
+        for (int i = 0; i < MA; ++i)
+#pragma unroll
+          for (int j = 0; j < nj(i); ++j) {
+            const int rl = 32 * fa(i) + rr;
+            uint16_t *o = static_cast<uint16_t *>(bk_args()->out) + (int64_t)(row0 + rl) * ldo;
+#pragma unroll
+            for (int q = 0; q < QP; ++q) {
+              // quads q and q + QP: columns 8 q .. and 8 (q + QP) ..
+              uint32_t lo[2], hi[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int e = 4 * q + 2 * k, f = e + 4 * QP;
+                lo[k] = bf16_pair(acc[i][j][e], acc[i][j][e + 1]);
+                hi[k] = bf16_pair(acc[i][j][f], acc[i][j][f + 1]);
+              }
+              const Pair32 u = swap32(lo[0], hi[0]), v = swap32(lo[1], hi[1]);
+              const int c = col(j) + 8 * (q + QP * hh);
+              if (rl < nrows && c < ldo)
+                *reinterpret_cast<uint4 *>(o + c) = make_uint4(u.x, v.x, u.y, v.y);
             }
           }
       }
@@ -455,15 +522,15 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
     };
     auto pick = [&](auto self, auto n_c) __attribute__((always_inline)) {
       constexpr int n = decltype(n_c)::value;
-      if constexpr (n == 0) {
-        run(std::integral_constant<int, 0>{});
+      if constexpr (n == 1) {
+        run(std::integral_constant<int, 1>{});
       } else {
-        if (mtv == n) run(std::integral_constant<int, n>{});
+        if (nfr == n) run(std::integral_constant<int, n>{});
         else self(self, std::integral_constant<int, n - 1>{});
       }
     };
-    pick(pick, std::integral_constant<int, MF>{});
-    // the issue cursor is ns (<= nst) stages ahead: at the next tile
+    pick(pick, std::integral_constant<int, 2 * MF>{});
+    // the issue cursor is BK_NS (<= nst) stages ahead: at the next tile
     ct += nsl;
     cur = itl;
   }
@@ -473,23 +540,18 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
 constexpr double BK_TILE = 2.0;        // a tile's fixed time, in that of a 32-row fragment
 
 struct BlkPlan {
-  int mf, ns, grid, lds;
+  int mf, grid, lds;
   PnDeal deal;
 };
 
-inline BlkPlan blk_plan(int64_t rows, int E, int64_t N, int64_t K, int epilogue) {
+inline BlkPlan blk_plan(int64_t rows, int E, int64_t N, int epilogue) {
   BlkPlan pl{};
-  const int nst = std::max(2, (int)((K + FB - 1) / FB));
   const int ntn = (int)((N + PN_N - 1) / PN_N);
   const PnHeight h = pn_height(rows, E, ntn, BK_TILE, true, false, [&](int mf) {
-    if (mf > 2) return 0;
-    int ns = std::min(5, nst);
-    while (ns >= 2 && bk_layout(mf, ns, E).total > PN_LDS_MAX) --ns;
-    return ns;
+    return mf <= 2 && bk_layout(mf, E).total <= PN_LDS_MAX ? BK_NS : 0;
   });
   pl.mf = h.mf;
-  pl.ns = h.ns;
-  pl.lds = bk_layout(h.mf, h.ns, E).total;
+  pl.lds = bk_layout(h.mf, E).total;
   pl.grid = (int)std::min<int64_t>(256, qdt::tile_grid(rows, E, 64 * pl.mf, ntn));
   pl.deal = pn_deal(h, ntn, pl.grid);
   return pl;
@@ -502,8 +564,7 @@ void launch_blk_one(const BlkArgs &p, const BlkPlan &pl, hipStream_t s) {
                                                hipFuncAttributeMaxDynamicSharedMemorySize,
                                                PN_LDS_MAX) == hipSuccess;
   (void)attr;
-  hipLaunchKernelGGL(kern, dim3((unsigned)pl.grid), dim3(PN_THREADS), (size_t)pl.lds, s, p, pl.deal,
-                     pl.ns);
+  hipLaunchKernelGGL(kern, dim3((unsigned)pl.grid), dim3(PN_THREADS), (size_t)pl.lds, s, p, pl.deal);
 }
 template <int EPI>
 void launch_blk(const BlkArgs &p, const BlkPlan &pl, hipStream_t s) {
@@ -539,7 +600,7 @@ extern "C" qd_status moe_fp8_block_grouped_gemm(
   if (rows == 0) return QD_OK;
   BlkArgs p{a_codes, a_scales, a_rows, row_token, expert_offsets, E, rows, w_codes, w_scales,
             (int)N, (int)K, out, out_scales};
-  const BlkPlan pl = blk_plan(rows, E, N, K, epilogue);
+  const BlkPlan pl = blk_plan(rows, E, N, epilogue);
   hipStream_t s = qdh::S(stream);
   if (epilogue == QD_EPI_NONE) launch_blk<QD_EPI_NONE>(p, pl, s);
   else if (epilogue == QD_EPI_SWIGLU) launch_blk<QD_EPI_SWIGLU>(p, pl, s);
