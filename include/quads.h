@@ -416,6 +416,8 @@ qd_status qd_fp8_moe_layer_forward(const void *x, const float *logits, int64_t T
  *   topk_ids, topk_w, expert_offsets, row_token, inv_row : as
  *             moe_route_permute; rows from expert_offsets[E] on (there are k for
  *             each token that is not live) have row_token -1.
+ *   ws      : at least moe_route_scored_workspace(T, E, k) bytes (0 up to 256 tokens;
+ *             NULL is allowed there).
  *   1 <= k <= 32, k <= top_groups * (E / groups), E <= 1024, groups <= 64,
  *   E % groups == 0, scale finite.
  * ------------------------------------------------------------------- */

@@ -515,6 +515,33 @@ _EPILOGUES = {None: Q.QD_EPI_NONE, "none": Q.QD_EPI_NONE, "swiglu": Q.QD_EPI_SWI
               "swiglu_quant": Q.QD_EPI_SWIGLU_FP8}
 
 
+class _on:
+    """The device of the tensors as the current one (no cost where it is already)."""
+
+    def __init__(self, dev):
+        self.switch = None
+        if dev.index != torch.cuda.current_device():
+            self.switch = torch.cuda.device(dev)
+
+    def __enter__(self):
+        if self.switch is not None:
+            self.switch.__enter__()
+
+    def __exit__(self, *exc):
+        if self.switch is not None:
+            self.switch.__exit__(*exc)
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(dev):
+    """The current stream of a device, without building a Stream object for it."""
+    if _raw_stream is not None:
+        return _raw_stream(dev.index)
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
 def _need(t, name, dtypes, shape, device=None):
     """A tensor argument: on the GPU (that of the others), of one of the types and of
     the shape (None: any extent), its rows without gaps."""
@@ -569,18 +596,19 @@ def route_scored(logits, k, scoring="softmax", bias=None, groups=1, top_groups=1
     T, E = logits.shape
     dev = logits.device
     _router_tensors(bias, live, E, T, dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         ptr, ld = _rows_of(logits, "logits")
         ids = torch.empty((T, k), dtype=torch.int32, device=dev)
         w = torch.empty((T, k), dtype=torch.float32, device=dev)
         offs = torch.empty(E + 1, dtype=torch.int32, device=dev)
         row_token = torch.empty(T * k, dtype=torch.int32, device=dev)
         inv_row = torch.empty((T, k), dtype=torch.int32, device=dev)
-        ws = _ws(Q.lib().moe_route_scored_workspace(T, E, k), dev)
+        n = Q.lib().moe_route_scored_workspace(T, E, k)
+        ws = _ws(n, dev) if n else None
         Q.call("moe_route_scored_permute", ptr, _dtype(logits), ld, T, E, k, _scoring(scoring),
                _ptr(bias), groups, top_groups, group_sum, int(renorm), float(scale), _ptr(live),
                ids.data_ptr(), w.data_ptr(), offs.data_ptr(), row_token.data_ptr(),
-               inv_row.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+               inv_row.data_ptr(), _ptr(ws), n, _stream_of(dev))
     return ids, w, offs, row_token, inv_row
 
 
@@ -593,12 +621,12 @@ def route_scored_backward(logits, ids, grad_w, scoring="softmax", renorm=True, s
     k = ids.shape[-1]
     _dense(_need(ids, "ids", (torch.int32,), (T, k), dev), "ids")
     _dense(_need(grad_w, "grad_w", (torch.float32,), (T, k), dev), "grad_w")
-    with torch.cuda.device(dev):
+    with _on(dev):
         ptr, ld = _rows_of(logits, "logits")
         grad = torch.empty((T, E), dtype=logits.dtype, device=dev)
         Q.call("moe_route_scored_backward", ptr, _dtype(logits), ld, T, E, k, _scoring(scoring),
                int(renorm), float(scale), ids.data_ptr(), grad_w.data_ptr(), grad.data_ptr(), E,
-               _stream())
+               _stream_of(dev))
     return grad
 
 
@@ -614,12 +642,13 @@ def fp8_block_quantize_act(x):
     scales [ceil(cols / 128)][rows])."""
     _need(x, "x", (torch.bfloat16, torch.float32), (None, None))
     rows, cols = x.shape
-    with torch.cuda.device(x.device):
+    dev = x.device
+    with _on(dev):
         ptr, ld = _rows_of(x, "x")
-        codes = torch.empty((rows, cols), dtype=torch.uint8, device=x.device)
-        scales = torch.empty((_blocks(cols), rows), dtype=torch.float32, device=x.device)
+        codes = torch.empty((rows, cols), dtype=torch.uint8, device=dev)
+        scales = torch.empty((_blocks(cols), rows), dtype=torch.float32, device=dev)
         Q.call("fp8_block_quantize_act", ptr, _dtype(x), rows, cols, ld, codes.data_ptr(),
-               scales.data_ptr(), _stream())
+               scales.data_ptr(), _stream_of(dev))
     return codes, scales
 
 
@@ -631,7 +660,7 @@ def fp8_block_quantize_weight(w, transposed=False):
     _need(w, "w", (torch.bfloat16, torch.float32), (None, None, None))
     dev = w.device
     E, N, K = w.shape
-    with torch.cuda.device(dev):
+    with _on(dev):
         codes = torch.empty((E, N, K), dtype=torch.uint8, device=dev)
         scales = torch.empty((E, _blocks(N), _blocks(K)), dtype=torch.float32, device=dev)
         ct = st = None
@@ -639,7 +668,7 @@ def fp8_block_quantize_weight(w, transposed=False):
             ct = torch.empty((E, K, N), dtype=torch.uint8, device=dev)
             st = torch.empty((E, _blocks(K), _blocks(N)), dtype=torch.float32, device=dev)
         Q.call("fp8_block_quantize_weight", _dense(w, "w"), _dtype(w), E, N, K, codes.data_ptr(),
-               scales.data_ptr(), _ptr(ct), _ptr(st), _stream())
+               scales.data_ptr(), _ptr(ct), _ptr(st), _stream_of(dev))
     return (codes, scales, ct, st) if transposed else (codes, scales)
 
 
@@ -674,7 +703,7 @@ def fp8_block_grouped_gemm(a_codes, a_scales, w_codes, w_scales, rows, row_token
     if offsets is not None:
         _dense(_need(offsets, "offsets", (torch.int32,), (E + 1,), dev), "offsets")
     epi = _EPILOGUES[epilogue]
-    with torch.cuda.device(dev):
+    with _on(dev):
         cols = N if epi == Q.QD_EPI_NONE else N // 2
         fp8 = epi == Q.QD_EPI_SWIGLU_FP8
         out = torch.empty((rows, cols), dtype=torch.uint8 if fp8 else torch.bfloat16, device=dev)
@@ -683,7 +712,7 @@ def fp8_block_grouped_gemm(a_codes, a_scales, w_codes, w_scales, rows, row_token
             scales = torch.empty((_blocks(cols), rows), dtype=torch.float32, device=dev)
         Q.call("moe_fp8_block_grouped_gemm", _dense(a_codes, "a_codes"),
                _dense(a_scales, "a_scales"), a_rows, _ptr(row_token), _ptr(offsets), E, rows, wp,
-               sp, N, K, epi, out.data_ptr(), _ptr(scales), _stream())
+               sp, N, K, epi, out.data_ptr(), _ptr(scales), _stream_of(dev))
     return (out, scales) if fp8 else out
 
 
@@ -716,14 +745,14 @@ class FP8BlockMoELayer:
         _dense(_need(x, "x", (torch.bfloat16,), (T, H), dev), "x")
         _dense(_need(logits, "logits", (torch.float32,), (T, E), dev), "logits")
         _router_tensors(None, live, E, T, dev)
-        with torch.cuda.device(dev):
+        with _on(dev):
             if y is None:
                 y = torch.empty((T, H), dtype=torch.bfloat16, device=dev)
             else:
                 _dense(_need(y, "y", (torch.bfloat16,), (T, H), dev), "y")
             Q.call("qd_fp8_block_moe_layer_forward", x.data_ptr(), logits.data_ptr(), T, H, E,
                    self.k, self.I, *self._route, _ptr(live), *self._w13, *self._w2, y.data_ptr(),
-                   self.ws.data_ptr(), self.ws.numel(), _stream())
+                   self.ws.data_ptr(), self.ws.numel(), _stream_of(dev))
         return y
 
 

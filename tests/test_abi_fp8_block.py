@@ -31,8 +31,8 @@ def route(**kw):
     (dict(groups=8, top=1, k=3), Q.QD_ERR_SHAPE), (dict(scale=float("inf")), Q.QD_ERR_SHAPE),
     (dict(scale=float("nan")), Q.QD_ERR_SHAPE), (dict(renorm=2), Q.QD_ERR_SHAPE),
     (dict(logits=None), Q.QD_ERR_NULL), (dict(offs=None), Q.QD_ERR_NULL),
-    (dict(inv=None), Q.QD_ERR_NULL), (dict(ws=None), Q.QD_ERR_WORKSPACE),
-    (dict(n=16), Q.QD_ERR_WORKSPACE), (dict(logits=P + 4), Q.QD_ERR_ALIGN),
+    (dict(inv=None), Q.QD_ERR_NULL), (dict(T=257, ws=None), Q.QD_ERR_WORKSPACE),
+    (dict(T=257, n=16), Q.QD_ERR_WORKSPACE), (dict(logits=P + 4), Q.QD_ERR_ALIGN),
     (dict(bias=P + 4), Q.QD_ERR_ALIGN), (dict(ws=P + 8), Q.QD_ERR_ALIGN),
 ])
 def test_route_refusals(kw, want):

@@ -109,6 +109,23 @@ def test_ties_and_extremes():
         check(ops.route_scored(lg, 8, **kw), ref)
 
 
+@pytest.mark.parametrize("E,groups", [(64, 1), (96, 4), (128, 8), (160, 5), (256, 8), (512, 16), (1024, 1)])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_scores_that_float32_cannot_tell_apart(E, groups, scoring):
+    """Neighbouring float32 logits at magnitudes where the float32 scores (and the
+    sums of two) of different experts coincide, and biases that move them back."""
+    rng = np.random.default_rng(E + groups)
+    T = 130
+    base = rng.choice([-9.0, 0.25, 3.0, 6.0], (T, 1)).astype(np.float32)
+    step = rng.integers(0, 9, (T, E)).astype(np.float32) * np.float32(2.0 ** -21)
+    lg = base + step * np.abs(base)
+    for bias in (np.zeros(E, np.float32), rng.choice([0, 2.0 ** -30, -2.0 ** -30], E).astype(np.float32)):
+        kw = dict(scoring=scoring, groups=groups, top_groups=max(1, groups // 2), group_sum=2)
+        ref = OB.route(lg, 8, bias=bias, **kw)
+        check(ops.route_scored(torch.from_numpy(lg).to(DEV), 8, bias=torch.from_numpy(bias).to(DEV),
+                               **kw), ref)
+
+
 def test_nan_stays_in_its_row():
     rng = np.random.default_rng(3)
     lg = torch.from_numpy(rng.standard_normal((9, 128)).astype(np.float32)).to(DEV)
