@@ -493,15 +493,19 @@ qd_status fp8_block_quantize_weight(const void *w, int32_t dtype, int64_t groups
  *                     fp8_block_quantize_act: out u8 [rows][I], out_scales f32
  *                     [ceil(I / 128)][rows].
  *   out_scales      : QD_EPI_SWIGLU_FP8 only (ignored otherwise, NULL allowed).
+ *   ws              : moe_fp8_block_grouped_gemm_workspace(...) bytes (a handful of rows
+ *                     with QD_EPI_SWIGLU_FP8 needs some; NULL allowed where it is 0).
  * K % 16 == 0, E <= 1024; activation codes and one expert's weights below 4 GiB
  * (otherwise QD_ERR_UNSUPPORTED).  Rows from expert_offsets[E] on are left as they were.
  * ------------------------------------------------------------------- */
+size_t    moe_fp8_block_grouped_gemm_workspace(int64_t rows, int64_t N, int64_t K, int32_t E,
+                                               int32_t epilogue);
 qd_status moe_fp8_block_grouped_gemm(const uint8_t *a_codes, const float *a_scales,
                                      int64_t a_rows, const int32_t *row_token,
                                      const int32_t *expert_offsets, int32_t E, int64_t rows,
                                      const uint8_t *w_codes, const float *w_scales, int64_t N,
                                      int64_t K, int32_t epilogue, void *out, float *out_scales,
-                                     void *stream);
+                                     void *ws, size_t ws_bytes, void *stream);
 
 /* qd_fp8_block_moe_layer_forward -- the FP8 layer with fine-grained scales: scored
  * routing, x quantised per 1 x 128, W13 with SwiGLU and the quantisation of h, W2, combine:

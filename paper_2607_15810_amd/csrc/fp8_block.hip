@@ -17,7 +17,7 @@ __global__ __launch_bounds__(256) void fp8_block_act_kernel(const T *__restrict_
                                                             int64_t cols, int64_t ld,
                                                             uint8_t *__restrict__ codes,
                                                             float *__restrict__ scales) {
-  fb_quantize_act_body<T>(blockIdx.x, blockIdx.y, x, rows, cols, ld, codes, scales);
+  fb_quantize_act_body<T>(blockIdx.x, blockIdx.y, x, rows, rows, cols, ld, codes, scales);
 }
 
 // One workgroup per 128 x 128 block: thread (row group tid / 16, lane tid % 16) keeps
@@ -162,7 +162,7 @@ extern "C" qd_status fp8_block_quantize_weight(const void *w, int32_t dtype, int
 // ---------------------------------------------------------------- layer
 namespace {
 struct BlockLayout {
-  size_t route, ids, wts, offs, row_token, inv_row, xc, xs, hc, hs, z, total;
+  size_t route, ids, wts, offs, row_token, inv_row, xc, xs, hc, hs, hw, z, hw_bytes, total;
 };
 BlockLayout block_layer_layout(int64_t T, int64_t H, int32_t E, int32_t k, int64_t I) {
   BlockLayout L{};
@@ -179,6 +179,8 @@ BlockLayout block_layer_layout(int64_t T, int64_t H, int32_t E, int32_t k, int64
   L.xs = take((size_t)T * ((H + FB - 1) / FB) * 4);
   L.hc = take(R * I);
   L.hs = take(R * ((I + FB - 1) / FB) * 4);
+  L.hw_bytes = moe_fp8_block_grouped_gemm_workspace(T * k, 2 * I, H, E, QD_EPI_SWIGLU_FP8);
+  L.hw = take(L.hw_bytes);
   L.z = take(R * H * 2);
   L.total = o;
   return L;
@@ -218,10 +220,10 @@ extern "C" qd_status qd_fp8_block_moe_layer_forward(
   float *hs = reinterpret_cast<float *>(b + L.hs);
   // the products' refusals come before the first launch
   qd_status st = moe_fp8_block_grouped_gemm(xc, xs, T, row_token, offs, E, 0, w13_codes, w13_scales,
-                                            2 * I, H, QD_EPI_SWIGLU_FP8, hc, hs, stream);
+                                            2 * I, H, QD_EPI_SWIGLU_FP8, hc, hs, nullptr, 0, stream);
   if (st) return st;
   st = moe_fp8_block_grouped_gemm(hc, hs, R, nullptr, offs, E, 0, w2_codes, w2_scales, H, I,
-                                  QD_EPI_NONE, b + L.z, nullptr, stream);
+                                  QD_EPI_NONE, b + L.z, nullptr, nullptr, 0, stream);
   if (st) return st;
   st = moe_route_scored_permute(logits, QD_DTYPE_F32, E, T, E, k, scoring, bias, groups, top_groups,
                                 group_sum, renorm, scale, live, ids, wts, offs, row_token, inv_row,
@@ -230,10 +232,10 @@ extern "C" qd_status qd_fp8_block_moe_layer_forward(
   st = fp8_block_quantize_act(x, QD_DTYPE_BF16, T, H, H, xc, xs, stream);
   if (st) return st;
   st = moe_fp8_block_grouped_gemm(xc, xs, T, row_token, offs, E, R, w13_codes, w13_scales, 2 * I, H,
-                                  QD_EPI_SWIGLU_FP8, hc, hs, stream);
+                                  QD_EPI_SWIGLU_FP8, hc, hs, b + L.hw, L.hw_bytes, stream);
   if (st) return st;
   st = moe_fp8_block_grouped_gemm(hc, hs, R, nullptr, offs, E, R, w2_codes, w2_scales, H, I,
-                                  QD_EPI_NONE, b + L.z, nullptr, stream);
+                                  QD_EPI_NONE, b + L.z, nullptr, nullptr, 0, stream);
   if (st) return st;
   return moe_unpermute_combine(b + L.z, inv_row, wts, T, k, H, y, stream);
 }

@@ -77,18 +77,19 @@ __device__ __forceinline__ uint2 eight_codes(const Eight<T> &v, float enc) {
                     fb_codes4(v.at(4), v.at(5), v.at(6), v.at(7), enc));
 }
 
-// One workgroup's part of the 1 x 128 quantiser: 16 rows (from 16 rb on) x four blocks
-// (from 4 cb on).  Sixteen lanes hold a block, so the 16 rows' scales of a block are
-// stored side by side.
+// One workgroup's part of the 1 x 128 quantiser: a row of each 16 lanes (from
+// rb * blockDim.x / 16 on) x four blocks (from 4 cb on), so that the scales of a block are
+// stored side by side.  Rows from `live` on are left alone.
 template <typename T>
 __device__ __forceinline__ void fb_quantize_act_body(int64_t rb, int cb, const T *__restrict__ x,
-                                                     int64_t rows, int64_t cols, int64_t ld,
+                                                     int64_t rows, int64_t live, int64_t cols,
+                                                     int64_t ld,
                                                      uint8_t *__restrict__ codes,
                                                      float *__restrict__ scales) {
   constexpr int NB = 4;
   const int l = threadIdx.x & 15;
-  const int64_t r = rb * 16 + (threadIdx.x >> 4);
-  if (r >= rows) return;                 // whole rows of 16 lanes
+  const int64_t r = rb * (blockDim.x >> 4) + (threadIdx.x >> 4);
+  if (r >= live) return;                 // whole rows of 16 lanes
   const int nkb = (int)((cols + FB - 1) / FB);
   const int b0 = cb * NB;
   Eight<T> v[NB];

@@ -1,0 +1,70 @@
+// Operands and arithmetic that the two kernels of the FP8 block GEMM share.
+#pragma once
+#include "fp8_block_dev.h"
+
+namespace qdb {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct BlkArgs {
+  const uint8_t *a;            // [a_rows][K]
+  const float *a_scales;       // [KB][a_rows]
+  int64_t a_rows;
+  const int32_t *row_token;
+  const int32_t *offsets;
+  int E;
+  int64_t rows;
+  const uint8_t *w;            // [E][N][K]
+  const float *w_scales;       // [E][NB][KB]
+  int N, K;
+  void *out;                   // bf16 [rows][N or N / 2], or FP8 codes [rows][N / 2]
+  float *out_scales;           // [N / 256 rounded up][rows]
+};
+
+static __device__ const uint4 bk_zero = {0, 0, 0, 0};
+
+__device__ __forceinline__ f16x2 dec2(uint32_t w, bool hi) {
+  return hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true)
+            : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false);
+}
+// eight codes (two words) to f16, exact
+__device__ __forceinline__ f16x8 dec8(uint32_t lo, uint32_t hi) {
+  const f16x2 a = dec2(lo, false), b = dec2(lo, true), c = dec2(hi, false), d = dec2(hi, true);
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ float bk_swiglu(float g, float u) {
+  const float ex = __builtin_amdgcn_exp2f(-g * 1.4426950408889634f);
+  return g * __builtin_amdgcn_rcpf(1.0f + ex) * u;
+}
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
+}
+// The upper half of a against the lower half of b: with a and b the words of columns
+// 4 h .. and 16 + 4 h .. (h the lane's half) the two results are, for the lower lanes,
+// the words of columns 0 and 4, for the upper ones of 16 and 20.
+struct Pair32 { uint32_t x, y; };
+__device__ __forceinline__ Pair32 swap32(uint32_t a, uint32_t b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  return {r[0], r[1]};
+}
+
+// Weight row of row tb of a run of 32-row fragments that starts at output column c0 (0 past
+// the last: never stored); SwiGLU: a fragment is 16 gate rows and the 16 up rows of the
+// same columns.
+template <bool GLU>
+__device__ __forceinline__ int bk_wrow(int tb, int c0, int N) {
+  if (GLU) {
+    const int I = N >> 1, c = c0 + 16 * (tb >> 5) + (tb & 15);
+    return c < I ? c + (tb & 16 ? I : 0) : 0;
+  }
+  return c0 + tb < N ? c0 + tb : 0;
+}
+
+// gemm_block_few.hip: whether its kernel takes a call of these sizes, and the launch (h: f32
+// [rows][N / 2] of workspace with QD_EPI_SWIGLU_FP8)
+bool blk_few(int64_t rows, int E, int64_t N);
+void launch_blk_few(const BlkArgs &p, int epilogue, float *h, hipStream_t s);
+
+}  // namespace qdb

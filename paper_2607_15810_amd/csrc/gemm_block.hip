@@ -22,11 +22,13 @@
 //    them whatever n is.  The schedule is the NVFP4 panel kernel's (panel_sched.h): one
 //    persistent workgroup per CU, its tiles' stages one stream through an LDS ring
 //    filled by direct global->LDS loads.
+//  * Calls of a few rows, whose tiles would leave most CUs idle, run on the kernel of
+//    gemm_block_few.hip.
 //  * A stage is one block of K: 128 bytes of every row, the tile's row scales of that
 //    block and the scales of its weight fragments.  Pieces of 16 bytes past K come from a
 //    zero in memory.  The pieces of a row are placed by a row-dependent XOR, so the
 //    fragment reads are free of bank conflicts.  One barrier per stage.
-#include "fp8_block_dev.h"
+#include "gemm_block.h"
 #include "lds_dma.h"
 #include "panel_sched.h"
 #include "tile_sched.h"
@@ -36,52 +38,6 @@ namespace {
 using namespace qdb;
 using namespace qdl;
 using namespace qdp;
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-struct BlkArgs {
-  const uint8_t *a;            // [a_rows][K]
-  const float *a_scales;       // [KB][a_rows]
-  int64_t a_rows;
-  const int32_t *row_token;
-  const int32_t *offsets;
-  int E;
-  int64_t rows;
-  const uint8_t *w;            // [E][N][K]
-  const float *w_scales;       // [E][NB][KB]
-  int N, K;
-  void *out;                   // bf16 [rows][N or N / 2], or FP8 codes [rows][N / 2]
-  float *out_scales;           // [N / 256 rounded up][rows]
-};
-
-__device__ const uint4 bk_zero = {0, 0, 0, 0};
-
-__device__ __forceinline__ f16x2 dec2(uint32_t w, bool hi) {
-  return hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true)
-            : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false);
-}
-// eight codes (two words) to f16, exact
-__device__ __forceinline__ f16x8 dec8(uint32_t lo, uint32_t hi) {
-  const f16x2 a = dec2(lo, false), b = dec2(lo, true), c = dec2(hi, false), d = dec2(hi, true);
-  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-__device__ __forceinline__ float bk_swiglu(float g, float u) {
-  const float ex = __builtin_amdgcn_exp2f(-g * 1.4426950408889634f);
-  return g * __builtin_amdgcn_rcpf(1.0f + ex) * u;
-}
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
-  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-  typedef float f2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
-}
-// The upper half of a against the lower half of b: with a and b the words of columns
-// 4 h .. and 16 + 4 h .. (h the lane's half) the two results are, for the lower lanes,
-// the words of columns 0 and 4, for the upper ones of 16 and 20.
-struct Pair32 { uint32_t x, y; };
-__device__ __forceinline__ Pair32 swap32(uint32_t a, uint32_t b) {
-  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-  return {r[0], r[1]};
-}
 
 template <int MF>
 struct BkCfg {
@@ -123,18 +79,6 @@ __device__ __forceinline__ BkArgPtr bk_args() {
 // 16-byte piece c of tile row r sits at piece c ^ bk_swz(r) of the row's 128
 __device__ __forceinline__ int bk_swz(int r) { return (r >> 1) & 7; }
 
-// weight row of the tile's row tb (0 past the last: never stored); SwiGLU: a fragment of
-// 32 is 16 gate rows and the 16 up rows of the same columns
-template <bool GLU>
-__device__ __forceinline__ int bk_wrow(int tb, int nt, int N) {
-  if (GLU) {
-    const int I = N >> 1, c = nt * 128 + 16 * (tb >> 5) + (tb & 15);
-    return c < I ? c + (tb & 16 ? I : 0) : 0;
-  }
-  const int c = nt * PN_N + tb;
-  return c < N ? c : 0;
-}
-
 template <int MF, int EPI>
 __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, PnDeal deal) {
   using C = BkCfg<MF>;
@@ -145,6 +89,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   const int tid = threadIdx.x, lane = tid & 63, w = (int)uni((uint32_t)tid >> 6);
   const int N = p.N, E = p.E, K = p.K;
   const int KB = (K + FB - 1) / FB, NB = (N + FB - 1) / FB;
+  constexpr int NC = GLU ? 128 : PN_N;         // output columns of a tile
   const int nst = KB > BK_NS ? KB : BK_NS;     // a whole ring at least (zeros past K)
   const BkLayout L = bk_layout(MF, E);
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -196,7 +141,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
       oa[j] = src(rt, 8 * (wi + 8 * j) + (ln >> 3)) * (uint32_t)K + pc;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      ob[j] = (uint32_t)bk_wrow<GLU>(8 * (wi + 8 * j) + (ln >> 3), itl.nt, N) * (uint32_t)K + pc;
+      ob[j] = (uint32_t)bk_wrow<GLU>(8 * (wi + 8 * j) + (ln >> 3), NC * itl.nt, N) * (uint32_t)K + pc;
     // the stage's scales: rows of the tile by waves 0 .. MF - 1, weights (lane f: the
     // tile's rows from 16 f on) by wave MF, a placeholder by the others
     if (wi < MF) {
@@ -204,7 +149,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
       os = src(rt, 64 * wi + ln) * 4u;
     } else {
       sb = reinterpret_cast<const uint8_t *>(uni_ptr(q->w_scales + (int64_t)itl.e * NB * KB));
-      os = wi == MF ? (uint32_t)(bk_wrow<GLU>(16 * (ln & 15), itl.nt, N) / FB) * (uint32_t)KB * 4u : 0u;
+      os = wi == MF ? (uint32_t)(bk_wrow<GLU>(16 * (ln & 15), NC * itl.nt, N) / FB) * (uint32_t)KB * 4u : 0u;
     }
     left = nst;
     if (it + nsl < t_end) {
@@ -574,11 +519,17 @@ void launch_blk(const BlkArgs &p, const BlkPlan &pl, hipStream_t s) {
 
 }  // namespace
 
+extern "C" size_t moe_fp8_block_grouped_gemm_workspace(int64_t rows, int64_t N, int64_t K, int32_t E,
+                                                       int32_t epilogue) {
+  if (rows <= 0 || N <= 0 || K <= 0 || E < 1 || epilogue != QD_EPI_SWIGLU_FP8) return 0;
+  return blk_few(rows, E, N) ? qdh::align_up((size_t)rows * (N / 2) * 4) : 0;
+}
+
 extern "C" qd_status moe_fp8_block_grouped_gemm(
     const uint8_t *a_codes, const float *a_scales, int64_t a_rows, const int32_t *row_token,
     const int32_t *expert_offsets, int32_t E, int64_t rows, const uint8_t *w_codes,
     const float *w_scales, int64_t N, int64_t K, int32_t epilogue, void *out, float *out_scales,
-    void *stream) {
+    void *ws, size_t ws_bytes, void *stream) {
   if (epilogue != QD_EPI_NONE && epilogue != QD_EPI_SWIGLU && epilogue != QD_EPI_SWIGLU_FP8)
     return QD_ERR_DTYPE;
   if (E < 1 || rows < 0 || a_rows < 0 || N <= 0 || K <= 0 || K % 16 != 0) return QD_ERR_SHAPE;
@@ -596,12 +547,19 @@ extern "C" qd_status moe_fp8_block_grouped_gemm(
   if (E > PN_EMAX || rows > 0x7fffffffLL || a_rows > 0x7fffffffLL || N > 0x3fffffffLL ||
       K > 0x3fffffffLL || (a_rows > rows ? a_rows : rows) + 1 > lim / K || N > (lim - 1) / K)
     return QD_ERR_UNSUPPORTED;
+  const size_t need = moe_fp8_block_grouped_gemm_workspace(rows, N, K, E, epilogue);
+  if (need > 0 && (!ws || ws_bytes < need)) return QD_ERR_WORKSPACE;
+  if (!qdh::aligned16(ws)) return QD_ERR_ALIGN;
   if (qdh::fault_injected()) return QD_ERR_HIP;
   if (rows == 0) return QD_OK;
   BlkArgs p{a_codes, a_scales, a_rows, row_token, expert_offsets, E, rows, w_codes, w_scales,
             (int)N, (int)K, out, out_scales};
-  const BlkPlan pl = blk_plan(rows, E, N, epilogue);
   hipStream_t s = qdh::S(stream);
+  if (blk_few(rows, E, N)) {
+    launch_blk_few(p, epilogue, static_cast<float *>(ws), s);
+    return qdh::check_launch();
+  }
+  const BlkPlan pl = blk_plan(rows, E, N, epilogue);
   if (epilogue == QD_EPI_NONE) launch_blk<QD_EPI_NONE>(p, pl, s);
   else if (epilogue == QD_EPI_SWIGLU) launch_blk<QD_EPI_SWIGLU>(p, pl, s);
   else launch_blk<QD_EPI_SWIGLU_FP8>(p, pl, s);

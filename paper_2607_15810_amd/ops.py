@@ -707,12 +707,15 @@ def fp8_block_grouped_gemm(a_codes, a_scales, w_codes, w_scales, rows, row_token
         cols = N if epi == Q.QD_EPI_NONE else N // 2
         fp8 = epi == Q.QD_EPI_SWIGLU_FP8
         out = torch.empty((rows, cols), dtype=torch.uint8 if fp8 else torch.bfloat16, device=dev)
-        scales = None
+        scales = ws = None
+        n = 0
         if fp8:
             scales = torch.empty((_blocks(cols), rows), dtype=torch.float32, device=dev)
+            n = Q.lib().moe_fp8_block_grouped_gemm_workspace(rows, N, K, E, epi)
+            ws = _ws(n, dev) if n else None
         Q.call("moe_fp8_block_grouped_gemm", _dense(a_codes, "a_codes"),
                _dense(a_scales, "a_scales"), a_rows, _ptr(row_token), _ptr(offsets), E, rows, wp,
-               sp, N, K, epi, out.data_ptr(), _ptr(scales), _stream_of(dev))
+               sp, N, K, epi, out.data_ptr(), _ptr(scales), _ptr(ws), n, _stream_of(dev))
     return (out, scales) if fp8 else out
 
 

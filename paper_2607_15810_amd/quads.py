@@ -112,7 +112,10 @@ SIGNATURES = {
                                           c_void_p, c_void_p, c_void_p, c_void_p]),
     "moe_fp8_block_grouped_gemm": (c_int, [c_void_p, c_void_p, c_int64, c_void_p, c_void_p,
                                            c_int32, c_int64, c_void_p, c_void_p, c_int64, c_int64,
-                                           c_int32, c_void_p, c_void_p, c_void_p]),
+                                           c_int32, c_void_p, c_void_p, c_void_p, c_size_t,
+                                           c_void_p]),
+    "moe_fp8_block_grouped_gemm_workspace": (c_size_t, [c_int64, c_int64, c_int64, c_int32,
+                                                        c_int32]),
     "qd_fp8_block_moe_layer_workspace": (c_size_t, [c_int64, c_int64, c_int32, c_int32, c_int64]),
     "qd_fp8_block_moe_layer_forward": (c_int, [c_void_p, c_void_p, c_int64, c_int64, c_int32,
                                                c_int32, c_int64, c_int32, c_void_p, c_int32,

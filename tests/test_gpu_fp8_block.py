@@ -167,7 +167,8 @@ GEMMS = [
     ([1], 8, 16), ([5], 40, 48), ([0, 3, 0, 1], 64, 128), ([33], 264, 144),
     ([64, 1, 0, 70], 256, 256), ([200, 31], 136, 400), ([7, 9, 300], 384, 640),
     ([32, 32], 512, 2048), ([2] * 40, 320, 272), ([129, 0, 65], 192, 1168), ([513], 128, 2880),
-    ([1] * 8, 1536, 2048), ([700, 20], 640, 768),
+    ([1] * 8, 1536, 2048), ([700, 20], 640, 768), ([70], 8, 16), ([90, 3], 64, 48),
+    ([17, 8, 0, 9], 704, 1168), ([2, 1], 128, 7168),
 ]
 IDS = ["_".join(map(str, c[0][:3])) + f"n{c[1]}k{c[2]}" for c in GEMMS]
 
@@ -210,9 +211,10 @@ def test_rows_behind_the_last_are_left(live, rows, epi):
     osc = torch.full((nb * rows + 128,), 5.0, device=DEV)
     o, s0 = out[1:], osc[64:]
     t = [up(v) for v in (a, sa, tok, offs, w, sw)]
+    ws = torch.full((1 << 16,), 0xFF, dtype=torch.uint8, device=DEV)
     Q.call("moe_fp8_block_grouped_gemm", t[0].data_ptr(), t[1].data_ptr(), rows, t[2].data_ptr(),
            t[3].data_ptr(), E, rows, t[4].data_ptr(), t[5].data_ptr(), N, K, epi, o.data_ptr(),
-           s0.data_ptr(), stream())
+           s0.data_ptr(), ws.data_ptr(), ws.numel(), stream())
     assert (out[0] == 0x5A).all() and (out[1 + live:] == 0x5A).all()
     assert (osc[:64] == 5.0).all() and (osc[64 + nb * rows:] == 5.0).all()
     sc = osc[64:64 + nb * rows].view(nb, rows)
