@@ -293,4 +293,13 @@ qd_status grouped_gemm_bitmap(const qd_nvfp4 *a, const int32_t *row_token,
                               const qd_nvfp4 *w, const qd_nvfp4 *rq, const uint32_t *bitmap,
                               int32_t Ks, int32_t *sel_out, int32_t epilogue, void *out,
                               float *amax_partials, hipStream_t stream);
+// moe_route_scored_permute, and where x is not NULL the quantisation of x (bf16 [T][cols],
+// cols % 16 == 0, 16-byte aligned) as by fp8_block_quantize_act in its first launch.
+qd_status route_scored(const void *logits, int32_t dtype, int64_t ld, int64_t T, int32_t E,
+                       int32_t k, int32_t scoring, const float *bias, int32_t groups,
+                       int32_t top_groups, int32_t group_sum, int32_t renorm, float scale,
+                       const uint8_t *live, int32_t *topk_ids, float *topk_w,
+                       int32_t *expert_offsets, int32_t *row_token, int32_t *inv_row, void *ws,
+                       size_t ws_bytes, const void *x, int64_t cols, uint8_t *x_codes,
+                       float *x_scales, void *stream);
 }  // namespace qdi

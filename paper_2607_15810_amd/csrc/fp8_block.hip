@@ -225,12 +225,10 @@ extern "C" qd_status qd_fp8_block_moe_layer_forward(
   st = moe_fp8_block_grouped_gemm(hc, hs, R, nullptr, offs, E, 0, w2_codes, w2_scales, H, I,
                                   QD_EPI_NONE, b + L.z, nullptr, nullptr, 0, stream);
   if (st) return st;
-  st = moe_route_scored_permute(logits, QD_DTYPE_F32, E, T, E, k, scoring, bias, groups, top_groups,
-                                group_sum, renorm, scale, live, ids, wts, offs, row_token, inv_row,
-                                b + L.route, moe_route_scored_workspace(T, E, k), stream);
+  st = qdi::route_scored(logits, QD_DTYPE_F32, E, T, E, k, scoring, bias, groups, top_groups,
+                         group_sum, renorm, scale, live, ids, wts, offs, row_token, inv_row,
+                         b + L.route, moe_route_scored_workspace(T, E, k), x, H, xc, xs, stream);
   if (st || T == 0) return st;
-  st = fp8_block_quantize_act(x, QD_DTYPE_BF16, T, H, H, xc, xs, stream);
-  if (st) return st;
   st = moe_fp8_block_grouped_gemm(xc, xs, T, row_token, offs, E, R, w13_codes, w13_scales, 2 * I, H,
                                   QD_EPI_SWIGLU_FP8, hc, hs, b + L.hw, L.hw_bytes, stream);
   if (st) return st;

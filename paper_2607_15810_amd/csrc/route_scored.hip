@@ -1,7 +1,11 @@
 // moe_route_scored_permute and moe_route_scored_backward (the choice: route_scored_dev.h).
 //
+// The layer's activations are quantised in the first launch, by workgroups of their own
+// behind the routing's.
+//
 // Up to 64 tokens the whole call is one workgroup of sixteen waves; up to 256 the
 // permutation is one; above, blocks of 256 tokens are counted and then placed.
+#include "fp8_block_dev.h"
 #include "route_scored_dev.h"
 
 namespace {
@@ -10,9 +14,28 @@ using namespace qds;
 
 constexpr int RS_BLK = 256;            // tokens of a ranking block
 
+// The quantisation of x beside the routing: workgroups from `first` on, nb of them for each
+// four blocks of columns (x NULL: none).
+struct ActBeside {
+  const uint16_t *x;
+  int64_t rows, cols;
+  uint8_t *codes;
+  float *scales;
+  int first, nb;
+};
+__device__ __forceinline__ bool act_beside(const ActBeside &a) {
+  const int b = (int)blockIdx.x - a.first;
+  if (b < 0) return false;
+  const int cb = b / a.nb;
+  qdb::fb_quantize_act_body<uint16_t>(b - cb * a.nb, cb, a.x, a.rows, a.rows, a.cols, a.cols, a.codes,
+                                      a.scales);
+  return true;
+}
+
 template <typename L, int PER>
-__global__ __launch_bounds__(256) void score_topk_kernel(ScoreArgs p, ScoreLanes sl) {
+__global__ __launch_bounds__(256) void score_topk_kernel(ScoreArgs p, ScoreLanes sl, ActBeside act) {
   extern __shared__ __align__(16) unsigned char rs_lds[];
+  if (act_beside(act)) return;
   const int wid = threadIdx.x >> 6;
   const int64_t t = (int64_t)blockIdx.x * 4 + wid;
   if (t < p.T)                                   // whole waves; no barriers inside
@@ -99,12 +122,13 @@ constexpr int RS_ONE = 64;             // tokens of the call in one workgroup
 
 template <typename L, int PER>
 __global__ __launch_bounds__(1024) void score_small_kernel(ScoreArgs p, ScoreLanes sl,
-                                                           int32_t *offsets,
+                                                           ActBeside act, int32_t *offsets,
                                                            int32_t *row_token, int32_t *inv_row) {
   extern __shared__ __align__(16) unsigned char rs_lds[];
   __shared__ uint32_t mask[RS_EMAX * (RS_ONE / 32)];
   __shared__ int32_t base[RS_EMAX], ids[RS_ONE * RS_KMAX];
   __shared__ int ws[16];
+  if (act_beside(act)) return;
   const int wid = threadIdx.x >> 6;
   for (int64_t t = wid; t < p.T; t += 16)
     rs_token<L, PER>(p, sl, t, reinterpret_cast<uint64_t *>(rs_lds) + (size_t)wid * p.E,
@@ -342,12 +366,14 @@ extern "C" size_t moe_route_scored_workspace(int64_t T, int32_t E, int32_t k) {
          qdh::align_up((size_t)T * (k > 0 ? k : 1) * 4);
 }
 
-extern "C" qd_status moe_route_scored_permute(
+namespace qdi {
+
+qd_status route_scored(
     const void *logits, int32_t dtype, int64_t ld, int64_t T, int32_t E, int32_t k,
     int32_t scoring, const float *bias, int32_t groups, int32_t top_groups, int32_t group_sum,
     int32_t renorm, float scale, const uint8_t *live, int32_t *topk_ids, float *topk_w,
     int32_t *expert_offsets, int32_t *row_token, int32_t *inv_row, void *ws, size_t ws_bytes,
-    void *stream) {
+    const void *x, int64_t cols, uint8_t *x_codes, float *x_scales, void *stream) {
   const qd_status bad = check_scoring(dtype, ld, T, E, k, scoring, renorm);
   if (bad) return bad;
   if (groups < 1 || groups > RS_GMAX || E % groups != 0 || top_groups < 1 || top_groups > groups ||
@@ -373,11 +399,19 @@ extern "C" qd_status moe_route_scored_permute(
   const bool bf16 = dtype == QD_DTYPE_BF16;
   const ScoreLanes sl = rs_lanes(E, groups);
   const size_t keys = sl.lq < 0 ? (size_t)E * 8 : 0;       // a wave's
-  if (T <= RS_ONE && keys <= 2048) {             // (its LDS stays below 64 KB)
+  // x's workgroups: a row for each 16 threads, four blocks of columns
+  const bool one = T <= RS_ONE && keys <= 2048;  // (its LDS stays below 64 KB)
+  const int64_t groups_of = one ? 1 : (T + 3) / 4, arows = one ? 64 : 16;
+  ActBeside act{static_cast<const uint16_t *>(x), T, cols, x_codes, x_scales, (int)groups_of,
+                (int)((T + arows - 1) / arows)};
+  const int64_t acts = x ? act.nb * ((cols + 4 * qdb::FB - 1) / (4 * qdb::FB)) : 0;
+  if (groups_of + acts > 0x7fffffffLL) return QD_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)(groups_of + acts));
+  if (one) {
     rs_by_width(sl.per, [&](auto w) {
       constexpr int PER = decltype(w)::value;
       hipLaunchKernelGGL((bf16 ? score_small_kernel<uint16_t, PER> : score_small_kernel<float, PER>),
-                         dim3(1), dim3(1024), 16 * keys, s, p, sl, expert_offsets, row_token,
+                         grid, dim3(1024), 16 * keys, s, p, sl, act, expert_offsets, row_token,
                          inv_row);
     });
     return qdh::check_launch();
@@ -385,7 +419,7 @@ extern "C" qd_status moe_route_scored_permute(
   rs_by_width(sl.per, [&](auto w) {
     constexpr int PER = decltype(w)::value;
     hipLaunchKernelGGL((bf16 ? score_topk_kernel<uint16_t, PER> : score_topk_kernel<float, PER>),
-                       dim3((unsigned)((T + 3) / 4)), dim3(256), 4 * keys, s, p, sl);
+                       grid, dim3(256), 4 * keys, s, p, sl, act);
   });
   if (T <= RS_BLK) {
     hipLaunchKernelGGL(score_permute_kernel, dim3(1), dim3(1024), 0, s, T, E, k, topk_ids,
@@ -401,6 +435,19 @@ extern "C" qd_status moe_route_scored_permute(
   hipLaunchKernelGGL(score_scatter_kernel, dim3(nblk), dim3(RS_BLK), 0, s, T, E, k, nblk, topk_ids,
                      counts, ranks, expert_offsets, row_token, inv_row);
   return qdh::check_launch();
+}
+
+}  // namespace qdi
+
+extern "C" qd_status moe_route_scored_permute(
+    const void *logits, int32_t dtype, int64_t ld, int64_t T, int32_t E, int32_t k,
+    int32_t scoring, const float *bias, int32_t groups, int32_t top_groups, int32_t group_sum,
+    int32_t renorm, float scale, const uint8_t *live, int32_t *topk_ids, float *topk_w,
+    int32_t *expert_offsets, int32_t *row_token, int32_t *inv_row, void *ws, size_t ws_bytes,
+    void *stream) {
+  return qdi::route_scored(logits, dtype, ld, T, E, k, scoring, bias, groups, top_groups, group_sum,
+                           renorm, scale, live, topk_ids, topk_w, expert_offsets, row_token, inv_row,
+                           ws, ws_bytes, nullptr, 0, nullptr, nullptr, stream);
 }
 
 extern "C" qd_status moe_route_scored_backward(const void *logits, int32_t dtype, int64_t ld,
