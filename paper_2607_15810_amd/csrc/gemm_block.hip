@@ -39,6 +39,22 @@ using namespace qdb;
 using namespace qdl;
 using namespace qdp;
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// eight codes (two words) times the power of two of sc, exact in bf16
+__device__ __forceinline__ bf16x8 dec8b(uint32_t lo, uint32_t hi, float sc) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, sc, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, sc, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, sc, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, sc, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// the mantissa of a scale, in [1, 2)
+__device__ __forceinline__ float bk_mant(float v) {
+  return __uint_as_float((__float_as_uint(v) & 0x007FFFFFu) | 0x3F800000u);
+}
+
 template <int MF>
 struct BkCfg {
   static constexpr int M = 64 * MF;
@@ -48,7 +64,7 @@ struct BkCfg {
   static constexpr int LPS = MF + 4 + 1;               // loads per wave and stage
 };
 
-constexpr int BK_NS = 3;             // stages of the ring
+__host__ __device__ constexpr int bk_ns(int mf) { return mf > 2 ? 2 : 3; }   // stages of the ring
 
 struct BkLayout {
   int tok, amax, dummy, offs, mpre, perm, total;
@@ -57,7 +73,7 @@ struct BkLayout {
 // epilogue), the target of placeholder loads, the tile schedule
 __host__ __device__ inline BkLayout bk_layout(int mf, int E) {
   BkLayout L{};
-  int o = BK_NS * (64 * mf * 128 + 32768 + (mf + 1) * 256);
+  int o = bk_ns(mf) * (64 * mf * 128 + 32768 + (mf + 1) * 256);
   auto take = [&](int bytes) { const int at = o; o += (bytes + 15) & ~15; return at; };
   L.tok = take(2 * 64 * mf * 4);
   L.amax = take(8 * 64 * mf * 4);
@@ -90,7 +106,8 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   const int N = p.N, E = p.E, K = p.K;
   const int KB = (K + FB - 1) / FB, NB = (N + FB - 1) / FB;
   constexpr int NC = GLU ? 128 : PN_N;         // output columns of a tile
-  const int nst = KB > BK_NS ? KB : BK_NS;     // a whole ring at least (zeros past K)
+  constexpr int NR = bk_ns(MF);
+  const int nst = KB > NR ? KB : NR;     // a whole ring at least (zeros past K)
   const BkLayout L = bk_layout(MF, E);
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   int32_t *offs = reinterpret_cast<int32_t *>(lds + L.offs);
@@ -207,11 +224,11 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
     wait_vm<0>();
     pn_barrier();
     bind();
-    for (int q = 0; q < BK_NS; ++q) {      // stages of this tile
+    for (int q = 0; q < NR; ++q) {      // stages of this tile
       --left;
       loads(uni(lds0 + q * C::SLOT));
     }
-    wait_vm<(BK_NS - 1) * C::LPS>();
+    wait_vm<(NR - 1) * C::LPS>();
     pn_barrier();
   }
   int slot = 0;
@@ -227,14 +244,19 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
       constexpr int MA = FULL + HALF, NJ = FULL > 0 ? 2 : 1;
       constexpr int ITEMS = 2 * MA;            // (half of the block, row fragment)
       constexpr int NS = GLU ? 2 : 1;          // scales of a fragment: gate and up halves
-      f32x16 acc[MA][2], part[MA][2];
+      f32x16 acc[MA][2];
+      float unit[MA][NS];
       auto nj = [](int i) { return i < FULL ? 2 : 1; };
 #pragma unroll
-      for (int i = 0; i < MA; ++i)
+      for (int i = 0; i < MA; ++i) {
 #pragma unroll
-        for (int j = 0; j < nj(i); ++j)
+        for (int g = 0; g < NS; ++g) unit[i][g] = 1.0f;
 #pragma unroll
-          for (int q = 0; q < 16; ++q) acc[i][j][q] = part[i][j][q] = 0.0f;
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (j < nj(i)) acc[i][j][q] = 0.0f;
+      }
       const int r = lane & 31, h = lane >> 5, sw = bk_swz(r);
       struct Op {
         uint4 c[2];
@@ -260,19 +282,19 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
                                                     (((4 * st + 2 * h + k) ^ sw) << 4));
         return o;
       };
-      auto step8 = [](const Op &o, int ks) __attribute__((always_inline)) -> f16x8 {
+      auto step8 = [](const Op &o, int ks, float sc) __attribute__((always_inline)) -> bf16x8 {
         const uint4 q = o.c[ks >> 1];
-        return (ks & 1) ? dec8(q.z, q.w) : dec8(q.x, q.y);
+        return (ks & 1) ? dec8b(q.z, q.w, sc) : dec8b(q.x, q.y, sc);
       };
       auto sync = [&]() __attribute__((always_inline)) -> uint32_t {
-        wait_vm<(BK_NS - 2) * C::LPS>();
+        wait_vm<(NR - 2) * C::LPS>();
         pn_barrier();
         const uint32_t at = uni(lds0 + slot * C::SLOT);
-        slot = slot + 1 == BK_NS ? 0 : slot + 1;
+        slot = slot + 1 == NR ? 0 : slot + 1;
         return at;
       };
       struct Scales {
-        float w[NS], r[MA];
+        float w[NS], r[MA], wl;                // wl: of this lane's weight row
       };
       auto rd_s = [&](const unsigned char *sl) __attribute__((always_inline)) -> Scales {
         const float *ss = reinterpret_cast<const float *>(sl + C::SOFF);
@@ -281,46 +303,54 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
         for (int g = 0; g < NS; ++g) o.w[g] = ss[64 * MF + 4 * wn + g];
 #pragma unroll
         for (int i = 0; i < MA; ++i) o.r[i] = ss[32 * fa(i) + r];
+        o.wl = ss[64 * MF + 4 * wn + (GLU ? (r >> 4) & 1 : 0)];
         return o;
       };
-      // quarter ks of a row fragment's partial sums into its totals
-      auto fold = [&](int i, int ks, const Scales &v) __attribute__((always_inline)) {
-        float sc[NS];
+      // quarter e of fragment i's sums to the unit of the block whose scales are v
+      float rho[NS];
+      auto rescale = [&](int i, int e, const Scales &v) __attribute__((always_inline)) {
+        if (e == 0) {
+          const float ma = bk_mant(v.r[i]);
 #pragma unroll
-        for (int g = 0; g < NS; ++g) sc[g] = v.r[i] * v.w[g];
+          for (int g = 0; g < NS; ++g) {
+            const float u = ma * bk_mant(v.w[g]);
+            rho[g] = unit[i][g] * __builtin_amdgcn_rcpf(u);
+            unit[i][g] = u;
+          }
+        }
         const int n = 4 * nj(i);
 #pragma unroll
-        for (int e = 0; e < n; ++e) {
-          const int j = (ks * n + e) >> 4, q = (ks * n + e) & 15;
-          acc[i][j][q] = __builtin_fmaf(part[i][j][q], sc[GLU ? q >> 3 : 0], acc[i][j][q]);
+        for (int k = 0; k < 8; ++k) {
+          const int j = (e * n + k) >> 4, q = (e * n + k) & 15;
+          if (k < n) acc[i][j & 1][q] *= rho[GLU ? q >> 3 : 0];
         }
         // here and not where the compiler would sink it, past the loop's branches
 #pragma unroll
-        for (int j = 0; j < nj(i); ++j)
-          if (j == (ks * n) >> 4 || j == (ks * n + n - 1) >> 4) asm volatile("" : "+v"(acc[i][j]));
+        for (int j = 0; j < 2; ++j)
+          if (j < nj(i))
+          if (j == (e * n) >> 4 || j == (e * n + n - 1) >> 4) asm volatile("" : "+v"(acc[i][j]));
       };
       // The stream of one wave: per k-step of 16 the MFMAs of its operands, beside them
-      // the decoding of the next step's and a quarter of a fold, held together by the
-      // scheduling barriers.  (Both waves of a SIMD run in step: VALU work in lumps
-      // leaves the matrix unit idle for both.)  Codes are read an item ahead; the
-      // workgroup's barrier stands before the last item, whose codes are in registers.
-      // The partial sums of fragment i are folded just before they start anew.
+      // the decoding of the next step's and a quarter of a rescaling, held together by
+      // the scheduling barriers.  Codes are read an item ahead; the workgroup's barrier
+      // stands before the last item, whose codes are in registers.  Fragment i is
+      // rescaled in the item before its block begins.
       Op bq[NJ];
       const unsigned char *s0 = lds + slot * C::SLOT;
       Op a = rd_a(s0, 0);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) bq[j] = rd_b(s0, 0, j);
-      Scales sv = rd_s(s0), sp;
+      Scales sv = rd_s(s0);
+      if constexpr (MA > 1) {
 #pragma unroll
-      for (int g = 0; g < NS; ++g) sp.w[g] = 0.0f;
+        for (int e = 0; e < 4; ++e) rescale(0, e, sv);
+      }
+      bf16x8 av = step8(a, 0, sv.r[0]), b[NJ][4];
 #pragma unroll
-      for (int i = 0; i < MA; ++i) sp.r[i] = 0.0f;
-      f16x8 av = step8(a, 0), b[NJ][4];
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) b[j][0] = step8(bq[j], 0);
+      for (int j = 0; j < NJ; ++j) b[j][0] = step8(bq[j], 0, sv.wl);
       for (int s = 0; s < nst; ++s) {
         const unsigned char *sl = lds + slot * C::SLOT;
-        Scales sn;
+        Scales sn = sv;
 #pragma unroll
         for (int n = 0; n < ITEMS; ++n) {
           const int st = n / MA, i = n % MA;
@@ -339,33 +369,33 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
           }
           if (MA == 1 && st == 0) {
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) fold(0, ks, sp);
+            for (int e = 0; e < 4; ++e) rescale(0, e, sv);
           }
 #pragma unroll
           for (int ks = 0; ks < 4; ++ks) {
             __builtin_amdgcn_sched_barrier(0);
-            f32x16 z;
 #pragma unroll
-            for (int q = 0; q < 16; ++q) z[q] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < nj(i); ++j)
-              part[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                  b[j][ks], av, st == 0 && ks == 0 ? z : part[i][j], 0, 0, 0);
+            for (int j = 0; j < 2; ++j)
+              if (j < nj(i))
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j][ks], av, acc[i][j], 0, 0, 0);
             if (ks < 3) {
-              av = step8(a, ks + 1);
+              av = step8(a, ks + 1, sv.r[i]);
               if (i == 0) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) b[j][ks + 1] = step8(bq[j], ks + 1);
+                for (int j = 0; j < NJ; ++j) b[j][ks + 1] = step8(bq[j], ks + 1, sv.wl);
               }
             } else {
-              av = step8(an, 0);
+              av = step8(an, 0, last ? sn.r[0] : sv.r[turn ? 0 : i + 1]);
               if (turn) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) b[j][0] = step8(bn[j], 0);
+                for (int j = 0; j < NJ; ++j) b[j][0] = step8(bn[j], 0, last ? sn.wl : sv.wl);
               }
             }
-            if (MA > 1 && last) fold(0, ks, sv);
-            if (st == 0 && !turn) fold(i + 1, ks, sp);
+            if (MA > 1 && last && s + 1 < nst) {   // (its scales have just been read)
+              if (ks > 0) rescale(0, ks - 1, sn);
+              if (ks == 3) rescale(0, 3, sn);
+            }
+            if (st == 0 && !turn) rescale(i + 1, ks, sv);
           }
           __builtin_amdgcn_sched_barrier(0);
           if (last) issue(at);
@@ -375,13 +405,15 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
             for (int j = 0; j < NJ; ++j) bq[j] = bn[j];
           }
         }
-        sp = sv;
         sv = sn;
       }
 #pragma unroll
-      for (int i = MA > 1 ? 1 : 0; i < MA; ++i)
+      for (int i = 0; i < MA; ++i)
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) fold(i, ks, sp);
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (j < nj(i)) acc[i][j][q] *= unit[i][GLU ? q >> 3 : 0];
       // ---- epilogue.  Element q of a fragment: its weight row 8 (q / 4) + 4 h + q % 4, row r
       // of the rows; with SwiGLU q and q + 8 are gate and up of column 8 (q / 4) + 4 h + q % 4
       // of 16.  Four consecutive columns are a quad; the halves of the wave swap quads, so that
@@ -392,10 +424,10 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
 #pragma unroll
         for (int i = 0; i < MA; ++i)
 #pragma unroll
-          for (int j = 0; j < nj(i); ++j)
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int q = 0; q < 8; ++q)
-              acc[i][j][q] = bk_swiglu(acc[i][j][q], acc[i][j][q + 8]);
+              if (j < nj(i)) acc[i][j][q] = bk_swiglu(acc[i][j][q], acc[i][j][q + 8]);
       }
       // first column of fragment j
       auto col = [&](int j) __attribute__((always_inline)) {
@@ -407,9 +439,10 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
         for (int i = 0; i < MA; ++i) {
           float m = 0.0f;
 #pragma unroll
-          for (int j = 0; j < nj(i); ++j)
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int q = 0; q < 8; ++q) m = fmaxf(m, fabsf(acc[i][j][q]));
+            for (int q = 0; q < 8; ++q)
+              if (j < nj(i)) m = fmaxf(m, fabsf(acc[i][j][q]));
           m = col(0) < ldo ? fmaxf(m, __shfl_xor(m, 32, 64)) : 0.0f;
           if (hh == 0) amax[(i < FULL ? wn : wn + 4 * wm) * C::M + 32 * fa(i) + rr] = m;
         }
@@ -426,7 +459,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
           const bool in = rl < nrows;
           uint8_t *o = static_cast<uint8_t *>(g->out) + (int64_t)(row0 + rl) * ldo;
 #pragma unroll
-          for (int j = 0; j < nj(i); ++j) {
+          for (int j = 0; j < 2; ++j) if (j < nj(i)) {
             const uint32_t q0 = fb_codes4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], enc);
             const uint32_t q1 = fb_codes4(acc[i][j][4], acc[i][j][5], acc[i][j][6], acc[i][j][7], enc);
             const Pair32 u = swap32(q0, q1);
@@ -441,7 +474,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
 #pragma unroll
         for (int i = 0; i < MA; ++i)
 #pragma unroll
-          for (int j = 0; j < nj(i); ++j) {
+          for (int j = 0; j < 2; ++j) if (j < nj(i)) {
             const int rl = 32 * fa(i) + rr;
             uint16_t *o = static_cast<uint16_t *>(bk_args()->out) + (int64_t)(row0 + rl) * ldo;
 #pragma unroll
@@ -475,7 +508,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
       }
     };
     pick(pick, std::integral_constant<int, 2 * MF>{});
-    // the issue cursor is BK_NS (<= nst) stages ahead: at the next tile
+    // the issue cursor is NR (<= nst) stages ahead: at the next tile
     ct += nsl;
     cur = itl;
   }
@@ -492,9 +525,17 @@ struct BlkPlan {
 inline BlkPlan blk_plan(int64_t rows, int E, int64_t N, int epilogue) {
   BlkPlan pl{};
   const int ntn = (int)((N + PN_N - 1) / PN_N);
-  const PnHeight h = pn_height(rows, E, ntn, BK_TILE, true, false, [&](int mf) {
-    return mf <= 2 && bk_layout(mf, E).total <= PN_LDS_MAX ? BK_NS : 0;
-  });
+  // the height with the least estimated time: rounds of the CUs times a tile's
+  const double mean = (double)rows / E, sd = std::max(0.5, sqrt(mean));
+  PnHeight h{};
+  for (const int mf : {1, 2, 4}) {
+    if (bk_layout(mf, E).total > PN_LDS_MAX) continue;
+    double var;
+    const double n = std::max(pn_tiles(mean, sd, E, 64.0 * mf, 0.0, &var), 1.0 / E);
+    const double t = pn_rounds(n * E, sqrt(var * E), ntn) * (BK_TILE + (mean / 32.0 + 0.5) / n);
+    if (h.mf == 0 || t < 0.995 * h.time)       // even: the lower, its ring is deeper
+      h = {mf, bk_ns(mf), std::max(1, (int)std::min(8.0, n + 0.5)), n * E, t};
+  }
   pl.mf = h.mf;
   pl.lds = bk_layout(h.mf, E).total;
   pl.grid = (int)std::min<int64_t>(256, qdt::tile_grid(rows, E, 64 * pl.mf, ntn));
@@ -513,7 +554,8 @@ void launch_blk_one(const BlkArgs &p, const BlkPlan &pl, hipStream_t s) {
 }
 template <int EPI>
 void launch_blk(const BlkArgs &p, const BlkPlan &pl, hipStream_t s) {
-  if (pl.mf == 2) launch_blk_one<2, EPI>(p, pl, s);
+  if (pl.mf == 4) launch_blk_one<4, EPI>(p, pl, s);
+  else if (pl.mf == 2) launch_blk_one<2, EPI>(p, pl, s);
   else launch_blk_one<1, EPI>(p, pl, s);
 }
 
