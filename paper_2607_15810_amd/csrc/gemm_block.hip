@@ -120,7 +120,12 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   const PnSched S{offs, mpre, perm, E, deal, (int)(blockIdx.x & 7)};
   const int nsl = gridDim.x >> 3;
   const int t_end = pn_walk(S);
+  // the workgroup's tiles: one of each run of nsl places of the walk, from alternate ends,
+  // since the tiles' heights descend (128 experts of 256 +- 16 rows: the longest of the
+  // XCD's CUs has 26 row fragments in five tiles, 29.5 from one end)
   int ct = blockIdx.x >> 3;                // the tile being multiplied
+  const int odd = 2 * (nsl - ct) - 1, even = 2 * ct + 1;   // steps to runs 1, 3, .. and 2, 4, ..
+  int cstep = odd, istep = odd;
   // two waves of a SIMD (w, w + 4) take different row halves
   const int wm = (w ^ (w >> 2)) & 1, wn = w >> 1;
 
@@ -169,8 +174,8 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
       os = wi == MF ? (uint32_t)(bk_wrow<GLU>(16 * (ln & 15), NC * itl.nt, N) / FB) * (uint32_t)KB * 4u : 0u;
     }
     left = nst;
-    if (it + nsl < t_end) {
-      nx = pn_locate<MF>(S, it + nsl, ecur, lane);
+    if (it + istep < t_end) {
+      nx = pn_locate<MF>(S, it + istep, ecur, lane);
       tok_dma(nx, ibuf ^ 1);
     }
   };
@@ -199,7 +204,8 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   };
   auto issue = [&](uint32_t at) __attribute__((always_inline)) {
     if (left == 0) {
-      it += nsl;
+      it += istep;
+      istep = odd + even - istep;
       if (it < t_end) {
         itl = nx;
         ibuf ^= 1;
@@ -509,7 +515,8 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
     };
     pick(pick, std::integral_constant<int, 2 * MF>{});
     // the issue cursor is NR (<= nst) stages ahead: at the next tile
-    ct += nsl;
+    ct += cstep;
+    cstep = odd + even - cstep;
     cur = itl;
   }
   wait_vm<0>();

@@ -169,6 +169,8 @@ GEMMS = [
     ([32, 32], 512, 2048), ([2] * 40, 320, 272), ([129, 0, 65], 192, 1168), ([513], 128, 2880),
     ([1] * 8, 1536, 2048), ([700, 20], 640, 768), ([70], 8, 16), ([90, 3], 64, 48),
     ([17, 8, 0, 9], 704, 1168), ([2, 1], 128, 7168),
+    # more tiles than CUs, of every height, walked from both ends
+    ([37 * e % 191 for e in range(60)], 2048, 144), ([97 * e % 301 for e in range(24)], 3584, 272),
 ]
 IDS = ["_".join(map(str, c[0][:3])) + f"n{c[1]}k{c[2]}" for c in GEMMS]
 
