@@ -107,6 +107,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   const int KB = (K + FB - 1) / FB, NB = (N + FB - 1) / FB;
   constexpr int NC = GLU ? 128 : PN_N;         // output columns of a tile
   constexpr int NR = bk_ns(MF);
+  const int ntn = (N + PN_N - 1) / PN_N;
   const int nst = KB > NR ? KB : NR;     // a whole ring at least (zeros past K)
   const BkLayout L = bk_layout(MF, E);
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -135,6 +136,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   const uint32_t dummy = lds0 + (uint32_t)L.dummy;
   int it = ct, left = 0, ecur = 0, ibuf = 0;
   PnTile itl{}, nx{};
+  int kb = 0;                              // the block of K of the next stage to load
   uint32_t oa[MF], ob[4], os = 0;
   const uint8_t *pa = nullptr, *wb = nullptr, *sb = nullptr;
   auto tok_dma = [&](const PnTile &tl, int buf) __attribute__((always_inline)) {
@@ -155,8 +157,14 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   auto bind = [&]() __attribute__((always_inline)) {
     const BkArgPtr q = bk_args();
     const int wi = pn_fresh_s(w), ln = pn_fresh(lane);
-    wb = uni_ptr(q->w + (int64_t)itl.e * N * K);
-    pa = uni_ptr(q->a);
+    // Where the tile starts in K.  Rows that lie a multiple of 4 KB apart put a block on a
+    // few memory channels, and workgroups that all start at block 0 meet there: each
+    // expert and weight-row tile has a place of its own (so that a row's bits depend on
+    // neither the batch nor the schedule).  128 experts of 16 rows, N = 1536: K = 4096
+    // 187 -> 150 us, K = 4224, from block 0 on, 152; 256 rows, K = 768: 141 from block 0, 147 spread.
+    kb = K % 4096 == 0 ? (int)uni((uint32_t)(13 * (itl.e * ntn + itl.nt)) % (uint32_t)KB) : 0;
+    wb = uni_ptr(q->w + (int64_t)itl.e * N * K + kb * FB);
+    pa = uni_ptr(q->a + kb * FB);
     const int32_t *rt = q->row_token;
 #pragma unroll
     for (int j = 0; j < MF; ++j)
@@ -167,10 +175,10 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
     // the stage's scales: rows of the tile by waves 0 .. MF - 1, weights (lane f: the
     // tile's rows from 16 f on) by wave MF, a placeholder by the others
     if (wi < MF) {
-      sb = reinterpret_cast<const uint8_t *>(uni_ptr(q->a_scales));
+      sb = reinterpret_cast<const uint8_t *>(uni_ptr(q->a_scales + kb * q->a_rows));
       os = src(rt, 64 * wi + ln) * 4u;
     } else {
-      sb = reinterpret_cast<const uint8_t *>(uni_ptr(q->w_scales + (int64_t)itl.e * NB * KB));
+      sb = reinterpret_cast<const uint8_t *>(uni_ptr(q->w_scales + (int64_t)itl.e * NB * KB + kb));
       os = wi == MF ? (uint32_t)(bk_wrow<GLU>(16 * (ln & 15), NC * itl.nt, N) / FB) * (uint32_t)KB * 4u : 0u;
     }
     left = nst;
@@ -182,14 +190,14 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   // a stage of loads into the slot at LDS address at, LPS per wave always
   // (placeholders past the last tile), so that the waits can count
   auto loads = [&](uint32_t at) __attribute__((always_inline)) {
-    const int kb = nst - 1 - left;             // left has been counted down
-    if ((kb + 1) * FB <= K) {
+    const bool none = nst - 1 - left >= KB;    // (left has been counted down) no block: zeros
+    if ((kb + 1) * FB <= K && !none) {
 #pragma unroll
       for (int j = 0; j < MF; ++j) dma16s(pa, oa[j], uni(at + (w + 8 * j) * 1024));
 #pragma unroll
       for (int j = 0; j < 4; ++j) dma16s(wb, ob[j], uni(at + C::BOFF + (w + 8 * j) * 1024));
-    } else {                                   // the last block is short: zeros past K
-      const bool in = kb * FB + (int)pc < K;
+    } else {                                   // a short block: zeros past K
+      const bool in = !none && kb * FB + (int)pc < K;
       const uint8_t *z = reinterpret_cast<const uint8_t *>(&bk_zero);
 #pragma unroll
       for (int j = 0; j < MF; ++j) dma16(in ? pa + oa[j] : z, uni(at + (w + 8 * j) * 1024));
@@ -198,9 +206,12 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
         dma16(in ? wb + ob[j] : z, uni(at + C::BOFF + (w + 8 * j) * 1024));
     }
     dma4s(sb, os, uni(w <= MF ? at + C::SOFF + w * 256 : dummy));
-    pa += FB;
-    wb += FB;
-    if (kb + 1 < KB) sb += w < MF ? bk_args()->a_rows * 4 : w == MF ? 4 : 0;
+    const int64_t step = w < MF ? bk_args()->a_rows * 4 : w == MF ? 4 : 0;
+    const int d = kb + 1 < KB ? 1 : 1 - KB;    // to the next block, round to the first
+    kb += d;
+    pa += d * FB;
+    wb += d * FB;
+    sb += d * step;
   };
   auto issue = [&](uint32_t at) __attribute__((always_inline)) {
     if (left == 0) {
