@@ -17,15 +17,13 @@ __device__ __forceinline__ void fb_scale(float m, float &enc, float &dec) {
   enc = m >= kZeroAmax ? 448.0f / m : 1.0f;
   dec = 1.0f / enc;
 }
-__device__ __forceinline__ float fb_clamp(float v) {      // keeps NaN
-  v = v > 448.0f ? 448.0f : v;
-  return v < -448.0f ? -448.0f : v;
-}
-// four codes, element 0 in the low byte
+// Four codes, element 0 in the low byte.  |x| <= m, so x enc is at most 448 (1 + 2^-23) before
+// its rounding, which the conversion takes to 448: the clamp of the definition needs no
+// instruction.
 __device__ __forceinline__ uint32_t fb_codes4(float a, float b, float c, float d, float enc) {
   int w = 0;
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(fb_clamp(a * enc), fb_clamp(b * enc), w, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(fb_clamp(c * enc), fb_clamp(d * enc), w, true);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(a * enc, b * enc, w, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c * enc, d * enc, w, true);
   return (uint32_t)w;
 }
 
