@@ -64,7 +64,7 @@ __device__ __forceinline__ int bk_wrow(int tb, int c0, int N) {
 
 // gemm_block_few.hip: whether its kernel takes a call of these sizes, and the launch (h: f32
 // [rows][N / 2] of workspace with QD_EPI_SWIGLU_FP8)
-bool blk_few(int64_t rows, int E, int64_t N);
+bool blk_few(int64_t rows, int E, int64_t N, int epilogue);
 void launch_blk_few(const BlkArgs &p, int epilogue, float *h, hipStream_t s);
 
 }  // namespace qdb

@@ -151,14 +151,16 @@ __global__ __launch_bounds__(256) void block_few_quantize_kernel(const float *__
 namespace qdb {
 
 // The 8-row tiles of the experts that the rows may reach times the large kernel's tiles
-// of 256 weight rows, up to which this kernel is ahead (graphs of ten calls, K = 2048, 1536
-// weight rows, quantised: 8 experts of a row 13.3 us against 18.7, 16 18.5 against 19.3, 24 27.1
-// against 22.6; K = 768, 2048 weight rows, bf16: 7.2 against 10.6, 16 experts 12.1 against 11.3;
-// one expert of 64 rows, 2048 x 2048: 10.3 against 22.5; of one, 4096 x 7168: 11.4 against 47).
-constexpr int64_t FW_TILES = 112, FW_MOST = 64;
-bool blk_few(int64_t rows, int E, int64_t N) {
+// of 256 weight rows, up to which this kernel is ahead.  Graphs of ten calls, here against
+// there: K = 2048, 1536 weight rows, quantised: 8 experts of a row 13.3 us against 18.7, 16
+// 18.5 against 19.3, 24 27.1 against 22.6; in bf16, 8 experts of 16 rows 14.3 against 20.2, of 32
+// 23.6 against 20.4; K = 768, 2048 weight rows, bf16: 8 experts of a row 7.2 against 10.6, 16 12.1
+// against 11.3; one expert, 2048 x 2048: 64 rows 11.0 against 22.5, 100 16.6 against 23.8, 256 29.2
+// against 24.7; 4096 weight rows: 64 18.3 against 24.3, 100 27.4 against 24.4.
+constexpr int64_t FW_TILES = 128, FW_TILES_FP8 = 96, FW_MOST = 128;
+bool blk_few(int64_t rows, int E, int64_t N, int epilogue) {
   const int64_t ntn = (N + 255) / 256, mts = std::max<int64_t>((rows + 7) / 8, std::min<int64_t>(rows, E));
-  return rows <= FW_MOST && mts * ntn <= FW_TILES;
+  return rows <= FW_MOST && mts * ntn <= (epilogue == QD_EPI_SWIGLU_FP8 ? FW_TILES_FP8 : FW_TILES);
 }
 
 template <int EPI>
