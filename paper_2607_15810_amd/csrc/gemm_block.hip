@@ -5,14 +5,21 @@
 // Arithmetic.  The FP8 MFMAs add four products at a time and drop what lies more than
 // about twelve bits below the largest of them (measured against float64, K = 128: up to
 // 2^-12.5 of sum |products| from a 448 among values near 2^-4, on every fp8 and f8f6f4
-// shape), so a sum on them is no 32-bit sum.  Operands are decoded to f16 in registers
-// (v_cvt_scalef32_pk_f16_fp8, exact for every code) and multiplied on
-// v_mfma_f32_32x32x16_f16: 2^-22 on the same inputs, at the f16 rate.
+// shape), so a sum on them is no 32-bit sum.  Operands are decoded to bf16 in registers
+// and multiplied on v_mfma_f32_32x32x16_bf16, whose sums are (2^-22 on the same inputs),
+// at half the FP8 rate.
 //
-// A block's 128 products go into a partial sum, which one multiply-add per element
-// folds into the f32 total with the product of the two scales.  The weights are the
-// instruction's first operand, so a lane holds one activation row: its row scale is one
-// register, the weight scale is uniform, and the columns of a row leave a lane together.
+// Scales.  The conversion (v_cvt_scalef32_pk_bf16_fp8) takes a power of two for nothing, so
+// the exponents of both scales go into the operands, exactly.  What is left of a block is
+// the product u of the two mantissas, in [1, 4): the sums stand in units of the current
+// block's u and are multiplied by u_before / u once a block, one multiplication per element,
+// and once by u at the end.  (Partial sums of a block folded into a total by a
+// multiply-add cost the same instruction and a second set of accumulators, and those kept
+// tiles at 128 rows: 4096^3 137 -> 121 us.)  The unit's reciprocal is the hardware's: the
+// unit kept is the one multiplied by, off by less than 2^-22 a block.
+//
+// The weights are the instruction's first operand, so a lane holds one activation row: its
+// row scale is one register, and the columns of a row leave a lane together.
 //
 //  * Workgroup tile: up to 64 MF rows of one expert x 256 weight rows (SwiGLU: 128 gate
 //    rows and the matching up rows, one block of 128 of h; a fragment of 32 holds 16 of
@@ -22,6 +29,12 @@
 //    them whatever n is.  The schedule is the NVFP4 panel kernel's (panel_sched.h): one
 //    persistent workgroup per CU, its tiles' stages one stream through an LDS ring
 //    filled by direct global->LDS loads.
+//  * Bound, for hundreds of rows per expert, by the matrix unit and the vector unit beside
+//    it: 7 vector instructions per MFMA (decoding 3 to 4, rescaling 2), the matrix unit
+//    busy 51% of the cycles at 2.1 GHz (4096^3: 1.13 PFLOP/s; an isolated loop of the same
+//    instructions on random operands, which the chip's power limits, reaches 1.5), of
+//    experts 0.73 to 0.8 PFLOP/s (the epilogue, tiles of uneven height, weights from HBM).
+//    For tens of rows by HBM: 5.1 to 5.4 TB/s of weights.
 //  * Calls of a few rows, whose tiles would leave most CUs idle, run on the kernel of
 //    gemm_block_few.hip.
 //  * A stage is one block of K: 128 bytes of every row, the tile's row scales of that
@@ -50,9 +63,11 @@ __device__ __forceinline__ bf16x8 dec8b(uint32_t lo, uint32_t hi, float sc) {
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, sc, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// the mantissa of a scale, in [1, 2)
+// the mantissa of a scale with its sign, of size in [1, 2); NaN of a scale that is not finite
 __device__ __forceinline__ float bk_mant(float v) {
-  return __uint_as_float((__float_as_uint(v) & 0x007FFFFFu) | 0x3F800000u);
+  const uint32_t b = __float_as_uint(v);
+  const float m = __uint_as_float((b & 0x807FFFFFu) | 0x3F800000u);
+  return (b & 0x7F800000u) == 0x7F800000u ? __uint_as_float(0x7FC00000u) : m;
 }
 
 template <int MF>
@@ -107,8 +122,8 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
   const int KB = (K + FB - 1) / FB, NB = (N + FB - 1) / FB;
   constexpr int NC = GLU ? 128 : PN_N;         // output columns of a tile
   constexpr int NR = bk_ns(MF);
-  const int ntn = (N + PN_N - 1) / PN_N;
-  const int nst = KB > NR ? KB : NR;     // a whole ring at least (zeros past K)
+  const int nst = KB > 3 ? KB : 3;             // the deepest ring at least (zeros past K), at
+                                               // every height, so that bits do not differ
   const BkLayout L = bk_layout(MF, E);
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   int32_t *offs = reinterpret_cast<int32_t *>(lds + L.offs);
@@ -159,10 +174,11 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
     const int wi = pn_fresh_s(w), ln = pn_fresh(lane);
     // Where the tile starts in K.  Rows that lie a multiple of 4 KB apart put a block on a
     // few memory channels, and workgroups that all start at block 0 meet there: each
-    // expert and weight-row tile has a place of its own (so that a row's bits depend on
-    // neither the batch nor the schedule).  128 experts of 16 rows, N = 1536: K = 4096
-    // 187 -> 150 us, K = 4224, from block 0 on, 152; 256 rows, K = 768: 141 from block 0, 147 spread.
-    kb = K % 4096 == 0 ? (int)uni((uint32_t)(13 * (itl.e * ntn + itl.nt)) % (uint32_t)KB) : 0;
+    // weight-row tile has a place of its own.  (Not each expert too, which would be 1 to 3%
+    // faster still: a row's bits depend on neither the batch, the schedule nor the
+    // expert's number.)  128 experts of 16 rows, N = 1536: K = 4096 187 -> 154 us, K = 4224, from
+    // block 0 on, 152; 256 rows, K = 768: 141 from block 0, 147 spread.
+    kb = K % 4096 == 0 ? (int)uni((uint32_t)(13 * itl.nt) % (uint32_t)KB) : 0;
     wb = uni_ptr(q->w + (int64_t)itl.e * N * K + kb * FB);
     pa = uni_ptr(q->a + kb * FB);
     const int32_t *rt = q->row_token;
@@ -241,7 +257,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
     wait_vm<0>();
     pn_barrier();
     bind();
-    for (int q = 0; q < NR; ++q) {      // stages of this tile
+    for (int q = 0; q < NR; ++q) {         // stages of this tile (NR <= nst)
       --left;
       loads(uni(lds0 + q * C::SLOT));
     }

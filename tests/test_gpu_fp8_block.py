@@ -248,6 +248,84 @@ def test_scales_reach_their_blocks():
             assert y[r, n] == sa[r, r] * sw[0, n // 128, r]
 
 
+@pytest.mark.parametrize("rows", [3, 200])
+def test_scales_of_all_sizes(rows):
+    """Scales over 2^-60 .. 2^40, of either sign: a block's products under those of others."""
+    rng = np.random.default_rng(rows)
+    N, K = 192, 1040
+    a, sa, w, sw, _, offs, _ = make(rng, [rows], N, K, gather=False)
+    sa = (sa * 2.0 ** rng.integers(-50, 30, sa.shape) * rng.choice([-1, 1], sa.shape)).astype(np.float32)
+    sw = (sw * 2.0 ** rng.integers(-10, 10, sw.shape) * rng.choice([-1, 1], sw.shape)).astype(np.float32)
+    ref, mag = refs(a, sa, w, sw, None, offs)
+    check_bf16(ops.fp8_block_grouped_gemm(up(a), up(sa), up(w), up(sw), rows), ref, mag)
+
+
+@pytest.mark.parametrize("rows", [3, 200])
+def test_scales_of_zero_and_not_finite(rows):
+    rng = np.random.default_rng(rows)
+    N, K = 256, 400
+    a, sa, w, sw, _, offs, _ = make(rng, [rows], N, K, gather=False)
+    sa[1, 1] = 0.0                                 # a block that stands for zeros
+    ref, mag = refs(a, sa, w, sw, None, offs)
+    args = [up(a), up(sa), up(w), up(sw), rows]
+    check_bf16(ops.fp8_block_grouped_gemm(*args), ref, mag)
+    clean = ops.fp8_block_grouped_gemm(*args)
+    for bad in (float("nan"), float("inf")):
+        args[1][2, 0] = bad
+        y = ops.fp8_block_grouped_gemm(*args)
+        assert not torch.isfinite(y[0]).any() and torch.equal(y[1:], clean[1:])
+    args[1] = up(sa)
+    args[3][0, 1, 2] = float("nan")                # columns 128 .. 255
+    y = ops.fp8_block_grouped_gemm(*args)
+    assert torch.isnan(y[:, 128:]).all() and torch.equal(y[:, :128], clean[:, :128])
+
+
+def test_offsets_past_32_bits():
+    """Weights of 5 GiB (each expert below 4), an output of 5 GB, activations of 4.6 GB."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    E, N, K = 5, 16384, 65536
+    w = torch.randint(0, 0x7F, (E, N, K), dtype=torch.uint8, generator=g, device=DEV)
+    sw = torch.rand((E, N // 128, K // 128), generator=g, device=DEV) + 0.5
+    a = torch.randint(0, 0x7F, (6, K), dtype=torch.uint8, generator=g, device=DEV)
+    sa = torch.rand((K // 128, 6), generator=g, device=DEV) + 0.5
+    offs = torch.tensor([0, 1, 2, 3, 3, 6], dtype=torch.int32, device=DEV)
+    y = ops.fp8_block_grouped_gemm(a, sa, w, sw, 6, None, offs)
+    one = ops.fp8_block_grouped_gemm(a[3:].contiguous(), sa[:, 3:].contiguous(), w[4:].contiguous(),
+                                     sw[4:].contiguous(), 3)
+    # the call of one expert may run on the other kernel, whose sums have another order:
+    # every product is positive, so each result is within HALF + FLOOR of the exact sum
+    assert ((y[3:].double() - one.double()).abs() <= 2.1 * (HALF + FLOOR) * one.double()).all()
+    del w
+    rows, N, K = 1 << 20, 2560, 16
+    a = torch.randint(0, 0x7F, (rows, K), dtype=torch.uint8, generator=g, device=DEV)
+    sa = torch.rand((1, rows), generator=g, device=DEV)
+    w = torch.randint(0, 0x7F, (1, N, K), dtype=torch.uint8, generator=g, device=DEV)
+    sw = torch.rand((1, N // 128, 1), generator=g, device=DEV)
+    y = ops.fp8_block_grouped_gemm(a, sa, w, sw, rows)
+    last = ops.fp8_block_grouped_gemm(a[-300:].contiguous(), sa[:, -300:].contiguous(), w, sw, 300)
+    assert torch.equal(y[-300:], last)
+    del y
+    x = torch.randn((70016, 65536), dtype=torch.bfloat16, generator=g, device=DEV)
+    codes, scales = ops.fp8_block_quantize_act(x)
+    c, s = ops.fp8_block_quantize_act(x[-40:])
+    assert torch.equal(codes[-40:], c) and torch.equal(scales[:, -40:], s)
+
+
+def test_a_row_does_not_depend_on_the_batch():
+    """The bits of a row of the large kernel are the same in every tile height, at any place
+    and beside any other rows."""
+    rng = np.random.default_rng(8)
+    for N, K in ((512, 1040), (256, 4096)):
+        a, sa, w, sw, _, _, _ = make(rng, [700, 200], N, K, gather=False)
+        t = [up(v) for v in (a, sa, w, sw)]
+        whole = ops.fp8_block_grouped_gemm(*t, 900, None, up(np.array([0, 700, 900], np.int32)))
+        for n0, n1 in ((300, 200), (700, 130), (131, 0)):
+            tok = np.concatenate([np.arange(n0)[::-1], 700 + np.arange(n1)]).astype(np.int32)
+            y = ops.fp8_block_grouped_gemm(*t, n0 + n1, up(tok), up(np.array([0, n0, n0 + n1], np.int32)))
+            assert torch.equal(y, whole[up(tok).long()])
+
+
 def test_a_nan_row_stays_alone():
     rng = np.random.default_rng(4)
     a, sa, w, sw, tok, offs, rows = make(rng, [40, 30], 256, 256, gather=False)
