@@ -6,7 +6,7 @@
 // registers between the block's maximum and its codes) and written as 1 + 4/128 B; a
 // weight element likewise, with one more byte for the transposed copy, which goes
 // through LDS.
-#include "fp8_block_dev.h"
+#include "gemm_block.h"
 
 namespace {
 
@@ -229,6 +229,20 @@ extern "C" qd_status qd_fp8_block_moe_layer_forward(
                          group_sum, renorm, scale, live, ids, wts, offs, row_token, inv_row,
                          b + L.route, moe_route_scored_workspace(T, E, k), x, H, xc, xs, stream);
   if (st || T == 0) return st;
+  if (qdb::blk_few(R, E, 2 * I, QD_EPI_SWIGLU_FP8) && qdb::blk_few(R, E, H, QD_EPI_NONE)) {
+    // a handful of rows: h stays in float32 and the down product quantises it (the
+    // same codes): the layer of one token 29.7 -> 27.7 us
+    float *h = reinterpret_cast<float *>(b + L.hw);
+    const qdb::BlkArgs up{xc, xs, T, row_token, offs, E, R, w13_codes, w13_scales, (int)(2 * I), (int)H,
+                     hc, hs};
+    qdb::launch_blk_few(up, QD_EPI_SWIGLU_FP8, h, false, qdh::S(stream));
+    const qdb::BlkArgs down{hc, hs, R, nullptr, offs, E, R, w2_codes, w2_scales, (int)H, (int)I,
+                       b + L.z, nullptr};
+    qdb::launch_blk_few_h(down, h, qdh::S(stream));
+    st = qdh::check_launch();
+    if (st) return st;
+    return moe_unpermute_combine(b + L.z, inv_row, wts, T, k, H, y, stream);
+  }
   st = moe_fp8_block_grouped_gemm(xc, xs, T, row_token, offs, E, R, w13_codes, w13_scales, 2 * I, H,
                                   QD_EPI_SWIGLU_FP8, hc, hs, b + L.hw, L.hw_bytes, stream);
   if (st) return st;

@@ -63,8 +63,10 @@ __device__ __forceinline__ int bk_wrow(int tb, int c0, int N) {
 }
 
 // gemm_block_few.hip: whether its kernel takes a call of these sizes, and the launch (h: f32
-// [rows][N / 2] of workspace with QD_EPI_SWIGLU_FP8)
+// [rows][N / 2] of workspace with QD_EPI_SWIGLU_FP8; codes false: h is left there, not
+// quantised), and the product without an epilogue of rows that are quantised from such an h.
 bool blk_few(int64_t rows, int E, int64_t N, int epilogue);
-void launch_blk_few(const BlkArgs &p, int epilogue, float *h, hipStream_t s);
+void launch_blk_few(const BlkArgs &p, int epilogue, float *h, bool codes, hipStream_t s);
+void launch_blk_few_h(const BlkArgs &p, const float *h, hipStream_t s);
 
 }  // namespace qdb

@@ -632,7 +632,7 @@ extern "C" qd_status moe_fp8_block_grouped_gemm(
             (int)N, (int)K, out, out_scales};
   hipStream_t s = qdh::S(stream);
   if (blk_few(rows, E, N, epilogue)) {
-    launch_blk_few(p, epilogue, static_cast<float *>(ws), s);
+    launch_blk_few(p, epilogue, static_cast<float *>(ws), true, s);
     return qdh::check_launch();
   }
   const BlkPlan pl = blk_plan(rows, E, N, epilogue);

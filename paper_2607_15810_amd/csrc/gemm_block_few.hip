@@ -7,7 +7,8 @@
 // loads counted by hand, no barrier), with the operands decoded to f16 as in the large
 // kernel.  The waves' float32 sums are joined in LDS in wave order.  With the quantising
 // epilogue h goes to workspace in float32 and a second launch quantises it: a block of 128 of
-// h spans eight workgroups.  Bound by latency: launch, tile search, row indices, the first
+// h spans eight workgroups.  The layer's down product takes that h instead (HIN) and each
+// wave quantises the blocks it needs, a launch less.  Bound by latency: launch, tile search, row indices, the first
 // block, four to eight blocks a wave, the join.
 #include "gemm_block.h"
 #include "lds_dma.h"
@@ -22,13 +23,14 @@ using namespace qdl;
 constexpr int FW_ROWS = 8;             // rows of a tile
 constexpr int FW_NS = 3;               // ring slots of a wave
 constexpr int FW_A = 4096, FW_S = FW_A + 1024, FW_SLOT = FW_S + 256;
-constexpr int FW_LPS = 6;              // loads of a block
 
 __device__ __forceinline__ int fw_swz(int r) { return (r >> 1) & 7; }
 
-template <int EPI>
+// h: where h goes (QD_EPI_SWIGLU_FP8), or with HIN the rows, f32 [rows][K]
+template <int EPI, bool HIN>
 __global__ __launch_bounds__(256) void gemm_block_few_kernel(BlkArgs p, int nfr, float *h) {
   constexpr bool GLU = EPI != QD_EPI_NONE;
+  constexpr int LPS = HIN ? 5 : 6;                 // counted loads of a block
   extern __shared__ __align__(16) unsigned char lds[];
   __shared__ int sh_w[4], sh_t[4];
   const int tid = threadIdx.x, lane = tid & 63, w = (int)uni((uint32_t)tid >> 6);
@@ -57,29 +59,61 @@ __global__ __launch_bounds__(256) void gemm_block_few_kernel(BlkArgs p, int nfr,
   const uint8_t *ga = p.a + ra * K + pa;
   // scales: lanes 0 .. 7 the rows', lanes 8, 9 the weights' of rows 0 and 16
   const bool wsc = (lane & 8) != 0;
-  const float *gs = wsc ? p.w_scales + ((int64_t)tl.e * NB + bk_wrow<GLU>(16 * (lane & 1), c0, N) / FB) * KB
+  const float *gs = wsc || HIN ? p.w_scales + ((int64_t)tl.e * NB + bk_wrow<GLU>(16 * (lane & 1), c0, N) / FB) * KB
                         : p.a_scales + rs;
-  const int64_t sstep = wsc ? 1 : p.a_rows;
+  const int64_t sstep = wsc || HIN ? 1 : p.a_rows;
   const uint8_t *z = reinterpret_cast<const uint8_t *>(&bk_zero);
   auto issue = [&](int kb, int slot) __attribute__((always_inline)) {
     const uint32_t at = uni(ring + slot * FW_SLOT);
     const int k = kb * FB;                         // (past K: zeros; past KB: nothing is read)
 #pragma unroll
     for (int j = 0; j < 4; ++j) dma16(k + (int)pw[j] < K ? gw[j] + k : z, at + j * 1024);
-    dma16(k + (int)pa < K ? ga + k : z, at + FW_A);
+    if constexpr (!HIN) dma16(k + (int)pa < K ? ga + k : z, at + FW_A);
     dma4(gs + (kb < KB ? kb : KB - 1) * sstep, at + FW_S);
   };
   const int nb = (KB - w + 3) >> 2;                // blocks of this wave
   f32x16 acc;
 #pragma unroll
   for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
+  // HIN: this wave's next two blocks of the rows, eight elements of rows lane / 16 and
+  // 4 + lane / 16 each (asked for ahead of the counted loads, which their waits include)
+  Eight<float> ha[2][2];
+  auto load_h = [&](Eight<float> (&v)[2], int kb) __attribute__((always_inline)) {
+    const int k = kb * FB + 8 * (lane & 15);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int rr = 4 * q + (lane >> 4);
+      if (k < K) v[q].load(h + (int64_t)(tl.row0 + (rr < tl.nrows ? rr : 0)) * K + k);
+      else v[q].zero();
+    }
+  };
+  if constexpr (HIN) {
+    load_h(ha[0], w);
+    load_h(ha[1], w + 4);
+  }
 #pragma unroll
   for (int i = 0; i < FW_NS; ++i) issue(w + 4 * i, i);
   const int r = lane & 31, hh = lane >> 5, sw = fw_swz(r), sa = fw_swz(r & 7);
   int slot = 0;
   for (int i = 0; i < nb; ++i) {
-    wait_vm<(FW_NS - 1) * FW_LPS>();
-    const unsigned char *sl = lds + w * FW_NS * FW_SLOT + slot * FW_SLOT;
+    wait_vm<(FW_NS - 1) * LPS>();
+    unsigned char *sl = lds + w * FW_NS * FW_SLOT + slot * FW_SLOT;
+    if constexpr (HIN) {                           // codes and scales to where the loads put them
+      float *ss = reinterpret_cast<float *>(sl + FW_S);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int rr = 4 * q + (lane >> 4), c8 = lane & 15;
+        float enc, dec;
+        fb_scale(row16_max(eight_amax(ha[0][q])), enc, dec);
+        *reinterpret_cast<uint2 *>(sl + FW_A + rr * 128 + ((c8 >> 1 ^ fw_swz(rr)) << 4) + 8 * (c8 & 1)) =
+            eight_codes(ha[0][q], enc);
+        if (c8 == 0) ss[rr] = dec;
+      }
+      wait_lds();
+      ha[0][0] = ha[1][0];
+      ha[0][1] = ha[1][1];
+      load_h(ha[1], w + 4 * (i + 2));
+    }
     uint4 cw[4], ca[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -163,14 +197,14 @@ bool blk_few(int64_t rows, int E, int64_t N, int epilogue) {
   return rows <= FW_MOST && mts * ntn <= (epilogue == QD_EPI_SWIGLU_FP8 ? FW_TILES_FP8 : FW_TILES);
 }
 
-template <int EPI>
+template <int EPI, bool HIN>
 static void launch_few_one(const BlkArgs &p, float *h, hipStream_t s) {
   const int nfr = EPI == QD_EPI_NONE ? (p.N + 31) / 32 : (p.N / 2 + 15) / 16;
   // every tile has a row
   const int64_t most = std::min<int64_t>(p.rows, (p.rows + FW_ROWS - 1) / FW_ROWS + p.E);
   const int64_t grid = (most * nfr + 7) / 8 * 8;
   constexpr int LDS = 4 * FW_NS * FW_SLOT;
-  auto kern = gemm_block_few_kernel<EPI>;
+  auto kern = gemm_block_few_kernel<EPI, HIN>;
   static const bool attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
                                                hipFuncAttributeMaxDynamicSharedMemorySize,
                                                LDS) == hipSuccess;
@@ -178,19 +212,24 @@ static void launch_few_one(const BlkArgs &p, float *h, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), LDS, s, p, nfr, h);
 }
 
-void launch_blk_few(const BlkArgs &p, int epilogue, float *h, hipStream_t s) {
+void launch_blk_few(const BlkArgs &p, int epilogue, float *h, bool codes, hipStream_t s) {
   if (epilogue == QD_EPI_NONE) {
-    launch_few_one<QD_EPI_NONE>(p, h, s);
+    launch_few_one<QD_EPI_NONE, false>(p, h, s);
   } else if (epilogue == QD_EPI_SWIGLU) {
-    launch_few_one<QD_EPI_SWIGLU>(p, h, s);
+    launch_few_one<QD_EPI_SWIGLU, false>(p, h, s);
   } else {
-    launch_few_one<QD_EPI_SWIGLU_FP8>(p, h, s);
+    launch_few_one<QD_EPI_SWIGLU_FP8, false>(p, h, s);
+    if (!codes) return;
     const int I = p.N / 2;
     hipLaunchKernelGGL(block_few_quantize_kernel,
                        dim3((unsigned)((p.rows + 15) / 16), (unsigned)((I + 4 * FB - 1) / (4 * FB))),
                        dim3(256), 0, s, h, p.offsets, p.E, p.rows, I,
                        static_cast<uint8_t *>(p.out), p.out_scales);
   }
+}
+
+void launch_blk_few_h(const BlkArgs &p, const float *h, hipStream_t s) {
+  launch_few_one<QD_EPI_NONE, true>(p, const_cast<float *>(h), s);
 }
 
 }  // namespace qdb

@@ -510,6 +510,7 @@ class FP8MoELayer:
 
 # ---------------------------------------------------------------- scored routing
 
+_FLOATS = (torch.bfloat16, torch.float32)
 _SCORING = {"softmax": Q.QD_SCORE_SOFTMAX, "sigmoid": Q.QD_SCORE_SIGMOID}
 _EPILOGUES = {None: Q.QD_EPI_NONE, "none": Q.QD_EPI_NONE, "swiglu": Q.QD_EPI_SWIGLU,
               "swiglu_quant": Q.QD_EPI_SWIGLU_FP8}
@@ -543,13 +544,14 @@ def _stream_of(dev):
 
 
 def _need(t, name, dtypes, shape, device=None):
-    """A tensor argument: on the GPU (that of the others), of one of the types and of
-    the shape (None: any extent), its rows without gaps."""
-    _require_cuda(t)
+    """A tensor argument: on the GPU (that of the others), of one of the types, and of
+    the shape (a number: of as many dimensions)."""
+    if not t.is_cuda:
+        raise ValueError("libquads operates on GPU tensors")
     if t.dtype not in dtypes:
         raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if (t.dim() != shape) if shape.__class__ is int else (t.shape != shape):
+        raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
     return t
@@ -592,7 +594,7 @@ def route_scored(logits, k, scoring="softmax", bias=None, groups=1, top_groups=1
     only; the top_groups best of `groups` expert groups by the sum of their group_sum
     best; weights renormalised over the chosen and times scale.  live (uint8 or bool
     [T]): tokens with 0 take no expert.  Returns (ids, w, offsets, row_token, inv_row)."""
-    _need(logits, "logits", (torch.bfloat16, torch.float32), (None, None))
+    _need(logits, "logits", _FLOATS, 2)
     T, E = logits.shape
     dev = logits.device
     _router_tensors(bias, live, E, T, dev)
@@ -615,7 +617,7 @@ def route_scored(logits, k, scoring="softmax", bias=None, groups=1, top_groups=1
 def route_scored_backward(logits, ids, grad_w, scoring="softmax", renorm=True, scale=1.0):
     """The gradient of route_scored's logits (their type) from that of its weights
     (grad_w f32 [T][k]); ids as route_scored returned them."""
-    _need(logits, "logits", (torch.bfloat16, torch.float32), (None, None))
+    _need(logits, "logits", _FLOATS, 2)
     T, E = logits.shape
     dev = logits.device
     k = ids.shape[-1]
@@ -640,7 +642,7 @@ def fp8_block_quantize_act(x):
     """E4M3 codes with one f32 scale per 128 elements of a row of x ([rows][cols] bf16
     or f32, rows contiguous; cols % 16 == 0).  Returns (codes u8 [rows][cols],
     scales [ceil(cols / 128)][rows])."""
-    _need(x, "x", (torch.bfloat16, torch.float32), (None, None))
+    _need(x, "x", _FLOATS, 2)
     rows, cols = x.shape
     dev = x.device
     with _on(dev):
@@ -657,7 +659,7 @@ def fp8_block_quantize_weight(w, transposed=False):
     Returns (codes u8 [E][N][K], scales [E][ceil(N / 128)][ceil(K / 128)]) and, with
     transposed, the same bank as [E][K][N] (N % 16 == 0), which gives input gradients:
     (codes, scales, codes_t, scales_t)."""
-    _need(w, "w", (torch.bfloat16, torch.float32), (None, None, None))
+    _need(w, "w", _FLOATS, 3)
     dev = w.device
     E, N, K = w.shape
     with _on(dev):
@@ -673,7 +675,7 @@ def fp8_block_quantize_weight(w, transposed=False):
 
 
 def _block_bank(codes, scales, name, dev=None):
-    _need(codes, name, (torch.uint8,), (None, None, None), dev)
+    _need(codes, name, (torch.uint8,), 3, dev)
     E, N, K = codes.shape
     _need(scales, name + " scales", (torch.float32,), (E, _blocks(N), _blocks(K)), codes.device)
     return _dense(codes, name), _dense(scales, name + " scales")
@@ -687,7 +689,7 @@ def fp8_block_grouped_gemm(a_codes, a_scales, w_codes, w_scales, rows, row_token
     offsets[E] on are left as the allocation gave them."""
     if epilogue not in _EPILOGUES:
         raise ValueError(f"epilogue must be one of {list(_EPILOGUES)}, not {epilogue!r}")
-    _need(a_codes, "a_codes", (torch.uint8,), (None, None))
+    _need(a_codes, "a_codes", (torch.uint8,), 2)
     dev = a_codes.device
     a_rows, K = a_codes.shape
     _need(a_scales, "a_scales", (torch.float32,), (_blocks(K), a_rows), dev)
@@ -696,7 +698,7 @@ def fp8_block_grouped_gemm(a_codes, a_scales, w_codes, w_scales, rows, row_token
     if w_codes.shape[2] != K:
         raise ValueError(f"w_codes has K = {w_codes.shape[2]}, a_codes {K}")
     if row_token is not None:
-        _need(row_token, "row_token", (torch.int32,), (None,), dev)
+        _need(row_token, "row_token", (torch.int32,), 1, dev)
         if row_token.numel() < rows:
             raise ValueError("row_token has fewer than `rows` entries")
         _dense(row_token, "row_token")
