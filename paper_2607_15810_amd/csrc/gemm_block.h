@@ -1,5 +1,7 @@
 // Operands and arithmetic that the two kernels of the FP8 block GEMM share.
 #pragma once
+#include <atomic>
+
 #include "fp8_block_dev.h"
 
 namespace qdb {
@@ -60,6 +62,16 @@ __device__ __forceinline__ int bk_wrow(int tb, int c0, int N) {
     return c < I ? c + (tb & 16 ? I : 0) : 0;
   }
   return c0 + tb < N ? c0 + tb : 0;
+}
+
+// More than 64 KB of dynamic LDS for a kernel, once on each device (done: a bit a device).
+inline void blk_allow_lds(const void *kern, int bytes, std::atomic<uint64_t> &done) {
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return;
+  const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (bit && (done.load(std::memory_order_relaxed) & bit)) return;
+  if (hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess)
+    done.fetch_or(bit, std::memory_order_relaxed);
 }
 
 // gemm_block_few.hip: whether its kernel takes a call of these sizes, and the launch (h: f32

@@ -580,10 +580,8 @@ inline BlkPlan blk_plan(int64_t rows, int E, int64_t N, int epilogue) {
 template <int MF, int EPI>
 void launch_blk_one(const BlkArgs &p, const BlkPlan &pl, hipStream_t s) {
   auto kern = gemm_block_kernel<MF, EPI>;
-  static const bool attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize,
-                                               PN_LDS_MAX) == hipSuccess;
-  (void)attr;
+  static std::atomic<uint64_t> done{0};
+  blk_allow_lds(reinterpret_cast<const void *>(kern), PN_LDS_MAX, done);
   hipLaunchKernelGGL(kern, dim3((unsigned)pl.grid), dim3(PN_THREADS), (size_t)pl.lds, s, p, pl.deal);
 }
 template <int EPI>

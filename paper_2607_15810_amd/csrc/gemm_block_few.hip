@@ -205,10 +205,8 @@ static void launch_few_one(const BlkArgs &p, float *h, hipStream_t s) {
   const int64_t grid = (most * nfr + 7) / 8 * 8;
   constexpr int LDS = 4 * FW_NS * FW_SLOT;
   auto kern = gemm_block_few_kernel<EPI, HIN>;
-  static const bool attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize,
-                                               LDS) == hipSuccess;
-  (void)attr;
+  static std::atomic<uint64_t> done{0};
+  blk_allow_lds(reinterpret_cast<const void *>(kern), LDS, done);
   hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), LDS, s, p, nfr, h);
 }
 
