@@ -618,8 +618,9 @@ extern "C" qd_status moe_fp8_block_grouped_gemm(
       ((uintptr_t)row_token & 3u) || ((uintptr_t)expert_offsets & 3u))
     return QD_ERR_ALIGN;
   const int64_t lim = 1LL << 32;
-  if (E > PN_EMAX || rows > 0x7fffffffLL || a_rows > 0x7fffffffLL || N > 0x3fffffffLL ||
-      K > 0x3fffffffLL || (a_rows > rows ? a_rows : rows) + 1 > lim / K || N > (lim - 1) / K)
+  // (rows that are gathered: their indices' offsets are 32-bit too)
+  if (E > PN_EMAX || rows > 0x3fffffffLL || a_rows > 0x3fffffffLL || N > 0x3fffffffLL ||
+      K > 0x3fffffffLL || a_rows + 1 > lim / K || N > (lim - 1) / K)
     return QD_ERR_UNSUPPORTED;
   const size_t need = moe_fp8_block_grouped_gemm_workspace(rows, N, K, E, epilogue);
   if (need > 0 && (!ws || ws_bytes < need)) return QD_ERR_WORKSPACE;

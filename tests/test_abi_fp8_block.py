@@ -91,9 +91,18 @@ def gemm(**kw):
     (dict(epi=2, wsp=P + 8), Q.QD_ERR_ALIGN),
     (dict(E=1025), Q.QD_ERR_UNSUPPORTED), (dict(K=1 << 20, a_rows=4096), Q.QD_ERR_UNSUPPORTED),
     (dict(K=1 << 20, N=4096), Q.QD_ERR_UNSUPPORTED), (dict(rows=0, a=None, out=None), Q.QD_OK),
+    (dict(rows=1 << 30), Q.QD_ERR_UNSUPPORTED), (dict(a_rows=1 << 30, rows=0), Q.QD_ERR_UNSUPPORTED),
 ])
 def test_gemm_refusals(kw, want):
     assert gemm(**kw) == want
+
+
+def test_gathered_rows_may_be_more_than_the_codes_hold(monkeypatch):
+    """The 4 GiB are those of the activation codes, not of the rows that gather them: k
+    rows of a long token each."""
+    monkeypatch.setenv("QD_FAULT_INJECT", "launch")
+    assert gemm(a_rows=1 << 16, rows=1 << 19, K=1 << 13) == Q.QD_ERR_HIP
+    assert gemm(a_rows=1 << 19, rows=1 << 19, K=1 << 13) == Q.QD_ERR_UNSUPPORTED
 
 
 def test_layer_refusals():

@@ -169,6 +169,8 @@ GEMMS = [
     ([32, 32], 512, 2048), ([2] * 40, 320, 272), ([129, 0, 65], 192, 1168), ([513], 128, 2880),
     ([1] * 8, 1536, 2048), ([700, 20], 640, 768), ([70], 8, 16), ([90, 3], 64, 48),
     ([17, 8, 0, 9], 704, 1168), ([2, 1], 128, 7168),
+    # the most experts, one row or none
+    ([(e * 7 % 5 > 0) + (e % 97 == 3) for e in range(1024)], 64, 144),
     # more tiles than CUs, of every height, walked from both ends
     ([37 * e % 191 for e in range(60)], 2048, 144), ([97 * e % 301 for e in range(24)], 3584, 272),
 ]
@@ -261,6 +263,19 @@ def test_scales_of_all_sizes(rows):
 
 
 @pytest.mark.parametrize("rows", [3, 200])
+def test_scales_of_the_largest_and_smallest_sizes(rows):
+    """Rows of scales near 2^-125 and near 2^117 against weights of the opposite."""
+    rng = np.random.default_rng(rows)
+    N, K = 192, 528
+    for e in (-125, 117):
+        a, sa, w, sw, _, offs, _ = make(rng, [rows], N, K, gather=False)
+        sa = rng.uniform(1, 2, sa.shape).astype(np.float32) * np.float32(2.0 ** e)
+        sw = rng.uniform(1, 2, sw.shape).astype(np.float32) * np.float32(2.0 ** (-e - 8))
+        ref, mag = refs(a, sa, w, sw, None, offs)
+        check_bf16(ops.fp8_block_grouped_gemm(up(a), up(sa), up(w), up(sw), rows), ref, mag)
+
+
+@pytest.mark.parametrize("rows", [3, 200])
 def test_scales_of_zero_and_not_finite(rows):
     rng = np.random.default_rng(rows)
     N, K = 256, 400
@@ -305,7 +320,17 @@ def test_offsets_past_32_bits():
     y = ops.fp8_block_grouped_gemm(a, sa, w, sw, rows)
     last = ops.fp8_block_grouped_gemm(a[-300:].contiguous(), sa[:, -300:].contiguous(), w, sw, 300)
     assert torch.equal(y[-300:], last)
-    del y
+    del y, a
+    # k rows of each token: more than 4 GiB of codes if they were not gathered
+    rows, K = 140000, 32768
+    a = torch.randint(0, 0x7F, (7, K), dtype=torch.uint8, generator=g, device=DEV)
+    sa = torch.rand((K // 128, 7), generator=g, device=DEV)
+    w = torch.randint(0, 0x7F, (1, 64, K), dtype=torch.uint8, generator=g, device=DEV)
+    sw = torch.rand((1, 1, K // 128), generator=g, device=DEV)
+    tok = (torch.arange(rows, device=DEV) % 7).int()
+    y = ops.fp8_block_grouped_gemm(a, sa, w, sw, rows, tok)
+    assert torch.equal(y, y[:7].repeat(20000, 1))
+    del y, tok
     x = torch.randn((70016, 65536), dtype=torch.bfloat16, generator=g, device=DEV)
     codes, scales = ops.fp8_block_quantize_act(x)
     c, s = ops.fp8_block_quantize_act(x[-40:])
