@@ -229,7 +229,8 @@ extern "C" qd_status qd_fp8_block_moe_layer_forward(
                          group_sum, renorm, scale, live, ids, wts, offs, row_token, inv_row,
                          b + L.route, moe_route_scored_workspace(T, E, k), x, H, xc, xs, stream);
   if (st || T == 0) return st;
-  if (qdb::blk_few(R, E, 2 * I, QD_EPI_SWIGLU_FP8) && qdb::blk_few(R, E, H, QD_EPI_NONE)) {
+  if (qdb::blk_few_rows(R, E, 2 * I, H, QD_EPI_SWIGLU_FP8) == 8 &&
+      qdb::blk_few_rows(R, E, H, I, QD_EPI_NONE) == 8) {
     // a handful of rows: h stays in float32 and the down product quantises it (the
     // same codes): the layer of one token 29.7 -> 27.7 us
     float *h = reinterpret_cast<float *>(b + L.hw);

@@ -74,10 +74,11 @@ inline void blk_allow_lds(const void *kern, int bytes, std::atomic<uint64_t> &do
     done.fetch_or(bit, std::memory_order_relaxed);
 }
 
-// gemm_block_few.hip: whether its kernel takes a call of these sizes, and the launch (h: f32
-// [rows][N / 2] of workspace with QD_EPI_SWIGLU_FP8; codes false: h is left there, not
-// quantised), and the product without an epilogue of rows that are quantised from such an h.
-bool blk_few(int64_t rows, int E, int64_t N, int epilogue);
+// gemm_block_few.hip: the rows of a tile of its kernel for a call of these sizes (0: the
+// large kernel takes it), and the launch (h: f32 [rows][N / 2] of workspace with
+// QD_EPI_SWIGLU_FP8; codes false: h is left there, not quantised), and the product without an
+// epilogue of rows that are quantised from such an h.
+int blk_few_rows(int64_t rows, int E, int64_t N, int64_t K, int epilogue);
 void launch_blk_few(const BlkArgs &p, int epilogue, float *h, bool codes, hipStream_t s);
 void launch_blk_few_h(const BlkArgs &p, const float *h, hipStream_t s);
 

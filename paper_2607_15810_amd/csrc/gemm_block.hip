@@ -596,7 +596,7 @@ void launch_blk(const BlkArgs &p, const BlkPlan &pl, hipStream_t s) {
 extern "C" size_t moe_fp8_block_grouped_gemm_workspace(int64_t rows, int64_t N, int64_t K, int32_t E,
                                                        int32_t epilogue) {
   if (rows <= 0 || N <= 0 || K <= 0 || E < 1 || epilogue != QD_EPI_SWIGLU_FP8) return 0;
-  return blk_few(rows, E, N, epilogue) ? qdh::align_up((size_t)rows * (N / 2) * 4) : 0;
+  return blk_few_rows(rows, E, N, K, epilogue) ? qdh::align_up((size_t)rows * (N / 2) * 4) : 0;
 }
 
 extern "C" qd_status moe_fp8_block_grouped_gemm(
@@ -630,7 +630,7 @@ extern "C" qd_status moe_fp8_block_grouped_gemm(
   BlkArgs p{a_codes, a_scales, a_rows, row_token, expert_offsets, E, rows, w_codes, w_scales,
             (int)N, (int)K, out, out_scales};
   hipStream_t s = qdh::S(stream);
-  if (blk_few(rows, E, N, epilogue)) {
+  if (blk_few_rows(rows, E, N, K, epilogue)) {
     launch_blk_few(p, epilogue, static_cast<float *>(ws), true, s);
     return qdh::check_launch();
   }

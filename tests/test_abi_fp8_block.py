@@ -87,7 +87,8 @@ def gemm(**kw):
     (dict(w=None), Q.QD_ERR_NULL), (dict(out=None), Q.QD_ERR_NULL),
     (dict(epi=2, os=None), Q.QD_ERR_NULL), (dict(a=P + 4), Q.QD_ERR_ALIGN),
     (dict(out=P + 8), Q.QD_ERR_ALIGN), (dict(tok=P + 2), Q.QD_ERR_ALIGN),
-    (dict(epi=2, wsp=None), Q.QD_ERR_WORKSPACE), (dict(epi=2, n=64), Q.QD_ERR_WORKSPACE),
+    (dict(epi=2, K=512, rows=8, wsp=None), Q.QD_ERR_WORKSPACE),
+    (dict(epi=2, K=512, rows=8, n=64), Q.QD_ERR_WORKSPACE),
     (dict(epi=2, wsp=P + 8), Q.QD_ERR_ALIGN),
     (dict(E=1025), Q.QD_ERR_UNSUPPORTED), (dict(K=1 << 20, a_rows=4096), Q.QD_ERR_UNSUPPORTED),
     (dict(K=1 << 20, N=4096), Q.QD_ERR_UNSUPPORTED), (dict(rows=0, a=None, out=None), Q.QD_OK),

@@ -2,11 +2,16 @@
 the GPU against the float64 oracle.
 
 Codes and scales of the quantisers must be equal.  A product in bf16 is off by half a
-step of the result (2^-8) and by the float32 sums before it.  Those, with exact
-products: 128 of a block in steps of four, each rounding (or truncating) by at most 2^-23
-of the block's sum of |products|, 32 * 2^-23 = 2^-18; the product of the two scales,
-the fold and the running total once a block, 3 * 23 blocks * 2^-24 < 2^-17.8 at K = 2880.
-Together they stay below 2^-16.8 of the sum of |products|."""
+step of the result (2^-8) and by the float32 sums before it, whose products are exact.
+Of a few rows, blocks folded into a total: 128 products in steps of four, each rounding (or
+truncating) by at most 2^-23 of the block's sum of |products|, 32 * 2^-23 = 2^-18; the
+product of the two scales, the fold and the total once a block, 3 * 23 * 2^-24 < 2^-17.8 at
+K = 2880.  Of more, one sum over K = n products, rescaled once a block: the unit, its
+reciprocal (2^-23), their product and the multiplication, 5 * 2^-24 for each of the blocks
+still to come, half of 23 on average, 2^-18.1; n / 4 steps that round the sum so far by
+2^-23, which for products of either sign lies within 4 standard deviations, 4 * 1.25 / sqrt(n)
+of the sum of |products| at the end and half of that on average: 0.63 sqrt(n) 2^-23 < 2^-17.8.
+Either stays below 2^-16.8 of the sum of |products|."""
 
 import numpy as np
 import pytest
@@ -171,10 +176,14 @@ GEMMS = [
     ([17, 8, 0, 9], 704, 1168), ([2, 1], 128, 7168),
     # the most experts, one row or none
     ([(e * 7 % 5 > 0) + (e % 97 == 3) for e in range(1024)], 64, 144),
+    # enough workgroups or rows for the large kernel, at the same odd sizes
+    ([40 * e % 97 for e in range(60)], 264, 144), ([3 * (e % 3) for e in range(200)], 136, 16),
+    ([200, 31] * 20, 136, 400), ([7, 9, 300] * 30, 384, 640), ([129, 0, 65] * 16, 704, 1168),
+    ([513, 700], 2560, 2880), ([64, 1, 0, 70] * 20, 256, 256), ([700, 20] * 3, 640, 768),
     # more tiles than CUs, of every height, walked from both ends
     ([37 * e % 191 for e in range(60)], 2048, 144), ([97 * e % 301 for e in range(24)], 3584, 272),
 ]
-IDS = ["_".join(map(str, c[0][:3])) + f"n{c[1]}k{c[2]}" for c in GEMMS]
+IDS = ["_".join(map(str, c[0][:3])) + f"e{len(c[0])}n{c[1]}k{c[2]}" for c in GEMMS]
 
 
 @pytest.mark.parametrize("case", GEMMS, ids=IDS)
@@ -200,7 +209,7 @@ def test_one_matrix_without_offsets():
     check_bf16(ops.fp8_block_grouped_gemm(up(a), up(sa), up(w), up(sw), rows), ref, mag)
 
 
-@pytest.mark.parametrize("live,rows", [(5, 8), (0, 40), (130, 300)])
+@pytest.mark.parametrize("live,rows", [(5, 8), (0, 40), (130, 300), (2600, 4000)])
 @pytest.mark.parametrize("epi", [Q.QD_EPI_NONE, Q.QD_EPI_SWIGLU, Q.QD_EPI_SWIGLU_FP8])
 def test_rows_behind_the_last_are_left(live, rows, epi):
     rng = np.random.default_rng(live)
@@ -215,7 +224,7 @@ def test_rows_behind_the_last_are_left(live, rows, epi):
     osc = torch.full((nb * rows + 128,), 5.0, device=DEV)
     o, s0 = out[1:], osc[64:]
     t = [up(v) for v in (a, sa, tok, offs, w, sw)]
-    ws = torch.full((1 << 16,), 0xFF, dtype=torch.uint8, device=DEV)
+    ws = torch.full((1 << 20,), 0xFF, dtype=torch.uint8, device=DEV)
     Q.call("moe_fp8_block_grouped_gemm", t[0].data_ptr(), t[1].data_ptr(), rows, t[2].data_ptr(),
            t[3].data_ptr(), E, rows, t[4].data_ptr(), t[5].data_ptr(), N, K, epi, o.data_ptr(),
            s0.data_ptr(), ws.data_ptr(), ws.numel(), stream())
@@ -250,7 +259,7 @@ def test_scales_reach_their_blocks():
             assert y[r, n] == sa[r, r] * sw[0, n // 128, r]
 
 
-@pytest.mark.parametrize("rows", [3, 200])
+@pytest.mark.parametrize("rows", [3, 200, 6000])
 def test_scales_of_all_sizes(rows):
     """Scales over 2^-60 .. 2^40, of either sign: a block's products under those of others."""
     rng = np.random.default_rng(rows)
@@ -262,7 +271,7 @@ def test_scales_of_all_sizes(rows):
     check_bf16(ops.fp8_block_grouped_gemm(up(a), up(sa), up(w), up(sw), rows), ref, mag)
 
 
-@pytest.mark.parametrize("rows", [3, 200])
+@pytest.mark.parametrize("rows", [3, 200, 6000])
 def test_scales_of_the_largest_and_smallest_sizes(rows):
     """Rows of scales near 2^-125 and near 2^117 against weights of the opposite."""
     rng = np.random.default_rng(rows)
@@ -275,7 +284,7 @@ def test_scales_of_the_largest_and_smallest_sizes(rows):
         check_bf16(ops.fp8_block_grouped_gemm(up(a), up(sa), up(w), up(sw), rows), ref, mag)
 
 
-@pytest.mark.parametrize("rows", [3, 200])
+@pytest.mark.parametrize("rows", [3, 200, 6000])
 def test_scales_of_zero_and_not_finite(rows):
     rng = np.random.default_rng(rows)
     N, K = 256, 400
@@ -337,29 +346,44 @@ def test_offsets_past_32_bits():
     assert torch.equal(codes[-40:], c) and torch.equal(scales[:, -40:], s)
 
 
-def test_a_row_does_not_depend_on_the_batch():
-    """The bits of a row of the large kernel are the same in every tile height, at any place
-    and beside any other rows."""
-    rng = np.random.default_rng(8)
-    for N, K in ((512, 1040), (256, 4096)):
-        a, sa, w, sw, _, _, _ = make(rng, [700, 200], N, K, gather=False)
-        t = [up(v) for v in (a, sa, w, sw)]
-        whole = ops.fp8_block_grouped_gemm(*t, 900, None, up(np.array([0, 700, 900], np.int32)))
-        for n0, n1 in ((300, 200), (700, 130), (131, 0)):
-            tok = np.concatenate([np.arange(n0)[::-1], 700 + np.arange(n1)]).astype(np.int32)
-            y = ops.fp8_block_grouped_gemm(*t, n0 + n1, up(tok), up(np.array([0, n0, n0 + n1], np.int32)))
-            assert torch.equal(y, whole[up(tok).long()])
+def random_codes(E, N, K, rows, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    code = lambda *n: torch.randint(0, 256, n, dtype=torch.uint8, generator=g, device=DEV) & 0xF7
+    scale = lambda *n: torch.rand(n, generator=g, device=DEV) + 0.5
+    return (code(rows, K), scale(-(-K // 128), rows), code(E, N, K),
+            scale(E, -(-N // 128), -(-K // 128)))
 
 
-def test_a_nan_row_stays_alone():
+# (the large kernel, in every tile height; the other, in both of its)
+@pytest.mark.parametrize("N,K,calls", [
+    (16384, 1040, [(300, 200), (700, 130), (131, 0)]), (16384, 4096, [(300, 200), (131, 0)]),
+    (256, 1040, [(1, 0), (3, 2), (40, 0), (131, 60)])])
+def test_a_row_does_not_depend_on_the_batch(N, K, calls):
+    """The bits of a row are the same in every tile height, at any place and beside any
+    other rows."""
+    t = random_codes(2, N, K, 900, 8)
+    first, rest = (700, 200) if N > 256 else (150, 60)
+    place = np.concatenate([np.arange(first), 700 + np.arange(rest)]).astype(np.int32)
+    whole = ops.fp8_block_grouped_gemm(*t, first + rest, up(place),
+                                       up(np.array([0, first, first + rest], np.int32)))
+    for n0, n1 in calls:
+        at = np.concatenate([np.arange(n0)[::-1], first + np.arange(n1)])
+        y = ops.fp8_block_grouped_gemm(*t, n0 + n1, up(place[at]),
+                                       up(np.array([0, n0, n0 + n1], np.int32)))
+        assert torch.equal(y, whole[up(at)])
+
+
+@pytest.mark.parametrize("counts", [[5, 2], [40, 30], [4000, 3000]])
+def test_a_nan_row_stays_alone(counts):
     rng = np.random.default_rng(4)
-    a, sa, w, sw, tok, offs, rows = make(rng, [40, 30], 256, 256, gather=False)
+    a, sa, w, sw, tok, offs, rows = make(rng, counts, 256, 256, gather=False)
     args = [up(a), up(sa), up(w), up(sw), rows, None, up(offs)]
     clean = ops.fp8_block_grouped_gemm(*args)
-    args[0][7, 100] = 0x7F
+    args[0][4, 100] = 0x7F
     y = ops.fp8_block_grouped_gemm(*args)
-    keep = [r for r in range(rows) if r != 7]
-    assert torch.isnan(y[7]).all() and torch.equal(y[keep], clean[keep])
+    keep = [r for r in range(rows) if r != 4]
+    assert torch.isnan(y[4]).all() and torch.equal(y[keep], clean[keep])
 
 
 def test_input_gradient():
@@ -408,6 +432,7 @@ LAYERS = [
     (64, 256, 160, 8, 2, dict(renorm=False)), (130, 400, 128, 6, 4, dict(bias=True)),
     (500, 512, 256, 4, 2, dict(scoring="sigmoid", bias=True, groups=2, top_groups=1)),
     (300, 1024, 384, 32, 8, dict(bias=True, groups=8, top_groups=4, group_sum=2)),
+    (2000, 512, 256, 16, 4, dict(bias=True)), (1500, 400, 96, 6, 4, dict(scoring="sigmoid")),
 ]
 
 
