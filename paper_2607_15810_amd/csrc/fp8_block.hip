@@ -5,7 +5,9 @@
 // Both quantisers are bound by HBM: an activation element is read once (2 B, kept in
 // registers between the block's maximum and its codes) and written as 1 + 4/128 B; a
 // weight element likewise, with one more byte for the transposed copy, which goes
-// through LDS.
+// through LDS.  5001 x 4096 activations 14.8 us with the launch (62 MB, 4.2 TB/s; a copy of
+// that size 4.9), 64 experts of 1536 x 2048 weights with the transposed copy 154 us (805 MB,
+// 5.2 TB/s).
 #include "gemm_block.h"
 
 namespace {

@@ -3,8 +3,14 @@
 // The layer's activations are quantised in the first launch, by workgroups of their own
 // behind the routing's.
 //
-// Up to 64 tokens the whole call is one workgroup of sixteen waves; up to 256 the
-// permutation is one; above, blocks of 256 tokens are counted and then placed.
+// Up to 64 tokens the whole call is one workgroup of sixteen waves (one token, 256 experts in
+// 8 groups: 6 us); up to 256 the permutation is one; above, blocks of 256 tokens are counted
+// and then placed.
+//
+// 8192 tokens, 256 experts in 8 groups, k = 8 (8.4 MB of f32 logits, 2 us of HBM): choice
+// 17.5 us, counts 4.7, placing 6.3.  The choice is bound by its instructions: a wave per
+// token, four of a workgroup, k + 1 rounds of a 64-lane maximum each waiting for the last.
+// The gradient, 4096 x 128 in bf16: 5.8 us, float64 exponentials of the chosen.
 #include "fp8_block_dev.h"
 #include "route_scored_dev.h"
 
