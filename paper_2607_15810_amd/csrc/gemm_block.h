@@ -51,6 +51,11 @@ __device__ __forceinline__ Pair32 swap32(uint32_t a, uint32_t b) {
   const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
   return {r[0], r[1]};
 }
+// The same between sixteens: lanes 16 .. 31 (48 .. 63) of a against lanes 0 .. 15 (32 .. 47) of b.
+__device__ __forceinline__ Pair32 swap16(uint32_t a, uint32_t b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  return {r[0], r[1]};
+}
 
 // Weight row of row tb of a run of 32-row fragments that starts at output column c0 (0 past
 // the last: never stored); SwiGLU: a fragment is 16 gate rows and the 16 up rows of the

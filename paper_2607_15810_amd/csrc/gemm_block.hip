@@ -450,7 +450,7 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
       // ---- epilogue.  Element q of a fragment: its weight row 8 (q / 4) + 4 h + q % 4, row r
       // of the rows; with SwiGLU q and q + 8 are gate and up of column 8 (q / 4) + 4 h + q % 4
       // of 16.  Four consecutive columns are a quad; the halves of the wave swap quads, so that
-      // a lane stores 8 or 16 consecutive columns.
+      // a lane stores 8 consecutive columns.
       const int ldo = pn_fresh_s(GLU ? N >> 1 : N);
       const int ln = pn_fresh(lane), rr = ln & 31, hh = ln >> 5;
       if constexpr (GLU) {
@@ -503,27 +503,37 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
             g->out_scales[(int64_t)nt * g->rows + row0 + rl] = dec;
         }
       } else {
-        constexpr int QP = GLU ? 1 : 2;        // pairs of quads of a fragment
+        // quads q and q + 1 of fragment j: columns 8 q .., of the wave's upper half 8 (q + 1) ..
+        auto pair = [&](int i, int j, int q) __attribute__((always_inline)) {
+          uint32_t lo[2], hi[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int e = 4 * q + 2 * k;
+            lo[k] = bf16_pair(acc[i][j][e], acc[i][j][e + 1]);
+            hi[k] = bf16_pair(acc[i][j][e + 4], acc[i][j][e + 5]);
+          }
+          const Pair32 u = swap32(lo[0], hi[0]), v = swap32(lo[1], hi[1]);
+          return make_uint4(u.x, v.x, u.y, v.y);
+        };
 #pragma unroll
         for (int i = 0; i < MA; ++i)
 #pragma unroll
           for (int j = 0; j < 2; ++j) if (j < nj(i)) {
-            const int rl = 32 * fa(i) + rr;
-            uint16_t *o = static_cast<uint16_t *>(bk_args()->out) + (int64_t)(row0 + rl) * ldo;
-#pragma unroll
-            for (int q = 0; q < QP; ++q) {
-              // quads q and q + QP: columns 8 q .. and 8 (q + QP) ..
-              uint32_t lo[2], hi[2];
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int e = 4 * q + 2 * k, f = e + 4 * QP;
-                lo[k] = bf16_pair(acc[i][j][e], acc[i][j][e + 1]);
-                hi[k] = bf16_pair(acc[i][j][f], acc[i][j][f + 1]);
-              }
-              const Pair32 u = swap32(lo[0], hi[0]), v = swap32(lo[1], hi[1]);
-              const int c = col(j) + 8 * (q + QP * hh);
+            uint16_t *out = static_cast<uint16_t *>(bk_args()->out);
+            auto put = [&](int rl, int c, uint4 v) __attribute__((always_inline)) {
               if (rl < nrows && c < ldo)
-                *reinterpret_cast<uint4 *>(o + c) = make_uint4(u.x, v.x, u.y, v.y);
+                *reinterpret_cast<uint4 *>(out + (int64_t)(row0 + rl) * ldo + c) = v;
+            };
+            if constexpr (GLU) {
+              put(32 * fa(i) + rr, col(j) + 8 * hh, pair(i, j, 0));
+            } else {
+              // both pairs of 16 rows in one store, so that it writes 64 bytes of each
+              const uint4 a = pair(i, j, 0), b = pair(i, j, 2);
+              const Pair32 x = swap16(a.x, b.x), y = swap16(a.y, b.y), z = swap16(a.z, b.z),
+                           w = swap16(a.w, b.w);
+              const int rl = 32 * fa(i) + (ln & 15), c = col(j) + 16 * ((ln >> 4) & 1) + 8 * hh;
+              put(rl, c, make_uint4(x.x, y.x, z.x, w.x));
+              put(rl + 16, c, make_uint4(x.y, y.y, z.y, w.y));
             }
           }
       }
