@@ -495,10 +495,10 @@ qd_status fp8_block_quantize_weight(const void *w, int32_t dtype, int64_t groups
  *                     fp8_block_quantize_act: out u8 [rows][I], out_scales f32
  *                     [ceil(I / 128)][rows].
  *   out_scales      : QD_EPI_SWIGLU_FP8 only (ignored otherwise, NULL allowed).
- *   ws              : moe_fp8_block_grouped_gemm_workspace(...) bytes (a handful of rows
- *                     with QD_EPI_SWIGLU_FP8 needs some; NULL allowed where it is 0).
- * K % 16 == 0, E <= 1024; activation codes and one expert's weights below 4 GiB
- * (otherwise QD_ERR_UNSUPPORTED).  Rows from expert_offsets[E] on are left as they were.
+ *   ws              : moe_fp8_block_grouped_gemm_workspace(...) bytes (up to some hundred
+ *                     rows with QD_EPI_SWIGLU_FP8 need some; NULL allowed where it is 0).
+ * K % 16 == 0, E <= 1024; activation codes and one expert's weights below 4 GiB, fewer than
+ * 2^30 rows (otherwise QD_ERR_UNSUPPORTED).  Rows from expert_offsets[E] on are left as they were.
  * ------------------------------------------------------------------- */
 size_t    moe_fp8_block_grouped_gemm_workspace(int64_t rows, int64_t N, int64_t K, int32_t E,
                                                int32_t epilogue);
