@@ -150,6 +150,18 @@ def test_no_tokens():
     assert g.shape == (0, 8)
 
 
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradient_of_one_renormalised_expert_is_zero(scoring, dtype):
+    """Its weight is the scale whatever the logits: no rounding is left in the gradient."""
+    lg = torch.randn((300, 96), device=DEV).to(dtype)
+    ids, w, *_ = ops.route_scored(lg, 1, scoring=scoring, scale=2.5)
+    assert (w == 2.5).all()
+    grad = ops.route_scored_backward(lg, ids, torch.randn((300, 1), device=DEV), scoring=scoring,
+                                     scale=2.5)
+    assert not grad.any()
+
+
 def test_gradient_leaves_the_gaps_between_rows():
     T, E, k, ld = 5, 24, 3, 40
     lg = torch.randn((T, E), device=DEV)
