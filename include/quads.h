@@ -406,9 +406,13 @@ qd_status qd_fp8_moe_layer_forward(const void *x, const float *logits, int64_t T
  * that of the logits; softmax scores are renormalised as a softmax over the
  * chosen logits.
  *   logits  : [T] rows of E elements of dtype (QD_DTYPE_BF16 or QD_DTYPE_F32), ld
- *             elements apart (ld >= E).  -inf is an expert with score 0; a NaN is
- *             chosen last (softmax: it makes the token's weights NaN), and the
- *             experts of a token are distinct and in range whatever the logits.
+ *             elements apart (ld >= E).  -inf is an expert with score 0.  A NaN is
+ *             chosen last (a group whose score it enters too), and the experts of a
+ *             token are distinct and in range whatever the logits.  Softmax: a NaN or
+ *             +inf among a token's E logits, chosen or not, makes its k weights NaN; the
+ *             choice is then made by the softmax of the numbers, of which +inf ones
+ *             share alike and leave the others 0.  Sigmoid: +inf scores 1, and only a
+ *             NaN that is chosen reaches the weights (with renorm all k of them).
  *   scoring : QD_SCORE_SOFTMAX or QD_SCORE_SIGMOID.
  *   bias    : f32 [E], or NULL.
  *   live    : uint8 [T], or NULL (every token is live).  A token with 0 takes no

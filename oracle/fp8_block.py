@@ -103,32 +103,55 @@ def scores(logits, scoring):
     if scoring == "sigmoid":
         return 1.0 / (1.0 + np.exp(-x))
     m = x.max(1, keepdims=True)
-    p = np.where(np.isneginf(m), 0.0, np.exp(x - np.where(np.isneginf(m), 0.0, m)))
+    with np.errstate(invalid="ignore"):          # a NaN or +inf: the whole row is NaN
+        p = np.where(np.isneginf(m), 0.0, np.exp(x - np.where(np.isneginf(m), 0.0, m)))
     z = p.sum(1, keepdims=True)
     return p / np.where(z == 0, 1.0, z)
+
+
+def choice_scores(logits, scoring):
+    """The scores that choose: those of `scores`, where it leaves numbers.  Of a softmax row
+    with a NaN or +inf, the softmax of its numbers, of which +inf ones share alike; a NaN
+    stays NaN."""
+    s = scores(logits, scoring)
+    x = np.asarray(logits, np.float64)
+    for t in range(x.shape[0]) if scoring == "softmax" else ():
+        num = ~np.isnan(x[t])
+        if num.all() and not np.isposinf(x[t]).any():
+            continue
+        s[t] = np.nan
+        if np.isposinf(x[t]).any():
+            top = np.isposinf(x[t])
+            s[t, num] = top[num] / top.sum()
+        elif num.any():
+            s[t, num] = scores(x[t:t + 1, num], scoring)[0]
+    return s
 
 
 def route(logits, k, scoring="softmax", bias=None, groups=1, top_groups=1, group_sum=1,
           renorm=True, scale=1.0, live=None):
     """S4, token by token: c = s + bias chooses (without bias and groups the logits do),
     the top_groups groups by the sum of their group_sum largest c, then the k largest c
-    of theirs; ties to the lower index; weight scale * s / sum(s chosen) or scale * s.
+    of theirs; ties to the lower index, a NaN after every number (`choice_scores`); weight
+    scale * s / sum(s chosen) or scale * s.
     Returns dict(ids, w, offsets, row_token, inv_row); w float64."""
     x = np.asarray(logits, np.float64)
     T, E = x.shape
     s = scores(x, scoring)
+    chooses = choice_scores(x, scoring)
     ids = np.full((T, k), -1, np.int64)
     w = np.zeros((T, k))
     n = E // groups
     for t in range(T):
         if live is not None and not live[t]:
             continue
-        c = list(x[t] if bias is None and groups == 1 else s[t] + (0.0 if bias is None else
-                                                                   np.asarray(bias, np.float64)))
-        part = sorted(range(groups), key=lambda g: (-sum(sorted(c[g * n:(g + 1) * n])[::-1][
-            :group_sum]), g))
+        c = list(x[t] if bias is None and groups == 1 else chooses[t] + (
+            0.0 if bias is None else np.asarray(bias, np.float64)))
+        first = lambda v: (np.isnan(v), 0.0 if np.isnan(v) else -v)
+        best = [sum(sorted(c[g * n:(g + 1) * n], key=first)[:group_sum]) for g in range(groups)]
+        part = sorted(range(groups), key=lambda g: (first(best[g]), g))
         pool = [e for g in part[:top_groups] for e in range(g * n, (g + 1) * n)]
-        ids[t] = sorted(pool, key=lambda e: (-c[e], e))[:k]
+        ids[t] = sorted(pool, key=lambda e: (first(c[e]), e))[:k]
         w[t] = s[t][ids[t]]
         if renorm:
             tot = w[t].sum()

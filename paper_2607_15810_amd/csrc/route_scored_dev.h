@@ -201,14 +201,17 @@ __device__ __forceinline__ void rs_choose_exact(const ScoreArgs &p, ScoreLanes s
     for (int j = 1; j < PER; ++j) m = fmaxf(m, x[j]);
     m = rs_wave_fmax(m);
     double z = 0.0;
+    // over the numbers: a NaN keeps its place, and of +inf logits each has the same share
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      s[j] = m == -INFINITY ? 0.0 : exp((double)x[j] - (double)m);
-      if (j < per && lane * per + j < E) z += s[j];
+      s[j] = x[j] == m ? 1.0 : exp((double)x[j] - (double)m);
+      if (m == -INFINITY) s[j] = 0.0;
+      if (x[j] != x[j]) s[j] = x[j];
+      else if (j < per && lane * per + j < E) z += s[j];
     }
     z = rs_wave_sum(z);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) s[j] = m == -INFINITY ? 0.0 : s[j] / z;
+    for (int j = 0; j < PER; ++j) s[j] = m == -INFINITY ? s[j] : s[j] / z;
   }
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
@@ -326,6 +329,14 @@ __device__ __forceinline__ void rs_token(const ScoreArgs &p, ScoreLanes sl, int6
     mx = rs_wave_fmax(mx);
   }
   const bool by_logit = !p.bias && p.G == 1;
+  // softmax: a NaN or +inf logit, chosen or not, leaves no score of the token a number.  Its
+  // weights are NaN; the choice is made over what is left (rs_choose_exact).
+  bool broken = false;
+  if (p.scoring == QD_SCORE_SOFTMAX) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) broken |= !(x[j] < INFINITY);
+    broken = __ballot(broken) != 0ull;
+  }
   constexpr float LOG2E = 1.4426950408889634f;
   if (by_logit) {
 #pragma unroll
@@ -352,7 +363,7 @@ __device__ __forceinline__ void rs_token(const ScoreArgs &p, ScoreLanes sl, int6
   }
 #pragma unroll
   for (int j = 0; j < PER; ++j) key[j] = j < per && lane * per + j < E ? rs_key(c[j]) : 0u;
-  bool sure = sl.lq >= 0;                        // uniform
+  bool sure = sl.lq >= 0 && (by_logit || !broken);   // uniform
   if (p.G > 1 && sure) {
     float a = -INFINITY, b = -INFINITY;          // the group's two largest
     bool nan = false;
@@ -487,6 +498,7 @@ __device__ __forceinline__ void rs_token(const ScoreArgs &p, ScoreLanes sl, int6
     const double n = rs_wave_sum(s);
     w = n == 0.0 ? 0.0 : w / n;
   }
+  if (broken) w = __longlong_as_double(0x7ff8000000000000ll);
   if (lane < k) {
     p.ids[t * k + lane] = my_e;
     p.wts[t * k + lane] = (float)w;

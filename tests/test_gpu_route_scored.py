@@ -200,3 +200,79 @@ def test_two_streams_and_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(out, w))
         assert torch.equal(ops.route_scored(src, k, **kw)[0], w[0])
+
+
+BROKEN = [
+    # T, E, k, router (bias: -3 on the last expert, so that +inf there is not chosen)
+    (13, 8, 3, dict()), (13, 8, 3, dict(bias=True)),
+    (64, 128, 8, dict(groups=8, top_groups=4, group_sum=2)),
+    (65, 128, 6, dict(bias=True, groups=4, top_groups=2, group_sum=1)),
+    (300, 256, 8, dict(bias=True, groups=8, top_groups=4, group_sum=2)),
+    (70, 60, 4, dict(bias=True, groups=20, top_groups=9, group_sum=2)),
+    (40, 96, 8, dict(groups=6, top_groups=2, group_sum=2)),
+    (26, 1024, 10, dict(bias=True)), (13, 513, 4, dict()),
+]
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("case", BROKEN, ids=[f"t{c[0]}_e{c[1]}_k{c[2]}" for c in BROKEN])
+def test_logits_that_are_no_numbers(case, dtype, scoring, renorm):
+    """A NaN is chosen after every number; a softmax row with a NaN or +inf anywhere has NaN
+    weights, and a choice of its numbers; no other row changes."""
+    T, E, k, kw = case
+    kw = dict(kw, scoring=scoring, renorm=renorm)
+    rng = np.random.default_rng(E + T)
+    x = rng.standard_normal((T, E)).astype(np.float32)
+    nan, inf = np.float32("nan"), np.float32("inf")
+    low = x.argmin(1)
+    for t in range(T):
+        at = t % 13
+        if at == 1:                                # on an expert that would not be chosen
+            x[t, low[t]] = nan
+        elif at == 2:
+            x[t, E - 1] = inf
+        elif at == 3:                              # on the one that would be first
+            x[t, x[t].argmax()] = nan
+        elif at == 4:
+            x[t, rng.permutation(E)[2:]] = nan
+        elif at == 5:
+            x[t] = nan
+        elif at == 6:
+            x[t, [1, E - 2]] = inf
+        elif at == 7:
+            x[t, 0], x[t, E // 2] = nan, inf
+        elif at == 8:
+            x[t] = -inf
+            x[t, 1] = nan
+        elif at == 9:
+            x[t] = -inf
+            x[t, 2] = inf
+        elif at == 10:                             # the lowest group of experts and some of the next
+            x[t, :E // 3] = nan
+        elif at == 11:
+            x[t] = inf
+    lg = torch.from_numpy(x).to(DEV).to(dtype)
+    b = None
+    if kw.pop("bias", False):
+        b = (0.1 * rng.standard_normal(E)).astype(np.float32)
+        b[E - 1] = -3.0
+    ref = OB.route(np_of(lg.float()), k, bias=b, **kw)
+    got = ops.route_scored(lg, k, bias=None if b is None else torch.from_numpy(b).to(DEV), **kw)
+    ids, w, offs, tok, inv = [np_of(t) for t in got]
+    assert np.array_equal(ids, ref["ids"])
+    assert np.array_equal(offs, ref["offsets"])
+    assert np.array_equal(tok, ref["row_token"]) and np.array_equal(inv, ref["inv_row"])
+    if scoring == "softmax":
+        broken = (np.isnan(x) | np.isposinf(x)).any(1)
+        assert np.isnan(w[broken]).all() and not np.isnan(w[~broken]).any()
+    assert np.array_equal(np.isnan(w), np.isnan(ref["w"]))
+    fine = ~np.isnan(w)
+    d = np.abs(w.astype(np.float64) - ref["w"])[fine]
+    assert (d <= ref["w"][fine] * 2.0 ** -23.99 + 2.0 ** -149).all()
+    # NaN after every number of the groups that take part
+    if kw.get("groups", 1) == 1:
+        numbers = (~np.isnan(x)).sum(1)
+        for t in range(T):
+            assert np.isnan(x[t, ids[t]]).sum() == max(0, k - numbers[t])

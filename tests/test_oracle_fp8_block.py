@@ -94,3 +94,23 @@ def test_dead_tokens_take_no_rows():
     r = OB.route(lg, 2, live=[1, 0, 1, 0, 0])
     assert r["offsets"][-1] == 4 and (r["ids"][[1, 3, 4]] == -1).all()
     assert (r["row_token"][4:] == -1).all() and set(r["row_token"][:4]) == {0, 2}
+
+
+def test_logits_that_are_no_numbers():
+    nan, inf = float("nan"), float("inf")
+    lg = np.array([[1, nan, 3, 2], [1, inf, 3, 2], [nan, nan, nan, 0], [nan, -inf, -inf, -inf],
+                   [inf, 0, inf, -inf]], np.float32)
+    # the choice passes over them, the softmax weights are NaN
+    r = OB.route(lg, 2, bias=np.zeros(4))
+    assert r["ids"].tolist() == [[2, 3], [1, 0], [3, 0], [1, 2], [0, 2]]
+    assert np.isnan(r["w"]).all()
+    assert OB.route(lg, 2)["ids"].tolist() == [[2, 3], [1, 2], [3, 0], [1, 2], [0, 2]]
+    # sigmoid: a NaN that is not chosen does no harm
+    r = OB.route(lg, 2, scoring="sigmoid")
+    assert np.isnan(r["w"]).any(1).tolist() == [False, False, True, False, False]
+    assert np.isnan(r["w"][2]).all()
+    # a group ranks by its numbers as far as they reach
+    lg = np.array([[5, nan, 0, 0], [nan, 4, 1, 1]], np.float32)
+    for gs, want in ((1, [[0], [1]]), (2, [[2], [2]])):
+        r = OB.route(lg, 1, scoring="sigmoid", groups=2, group_sum=gs)
+        assert r["ids"].tolist() == want
