@@ -297,6 +297,10 @@ __global__ __launch_bounds__(256) void score_grad_kernel(ScoreGradArgs p) {
     }
   }
   const bool on = id >= 0;
+  if (__ballot(on) == 0ull) {     // a dead token, whatever its logits
+    for (int e = lane; e < E; e += 64) rs_store<L>(p.grad, t * p.ldg + e, 0.0);
+    return;
+  }
   const bool full = p.scoring == QD_SCORE_SOFTMAX && !p.renorm;
   double d = 0.0;                 // this lane's chosen expert's gradient
   double dot = 0.0, z = 1.0;

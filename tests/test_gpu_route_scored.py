@@ -276,3 +276,28 @@ def test_logits_that_are_no_numbers(case, dtype, scoring, renorm):
         numbers = (~np.isnan(x)).sum(1)
         for t in range(T):
             assert np.isnan(x[t, ids[t]]).sum() == max(0, k - numbers[t])
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,E", [(9, 40), (300, 128), (12, 384)])
+def test_gradient_of_dead_tokens_over_stale_logits_is_zero(T, E, dtype, scoring, renorm):
+    """A batch padded to its graph's size: the logits behind the live tokens are anything."""
+    k = 3
+    lg = torch.randn((T, E), device=DEV).to(dtype)
+    live = torch.ones(T, dtype=torch.uint8, device=DEV)
+    live[T // 2:] = 0
+    clean = ops.route_scored(lg, k, scoring=scoring, renorm=renorm, live=live)
+    gw = torch.randn((T, k), device=DEV)
+    want = ops.route_scored_backward(lg, clean[0], gw, scoring=scoring, renorm=renorm)
+    bits_of = torch.int32 if dtype == torch.float32 else torch.int16
+    assert not want[T // 2:].view(bits_of).any()                  # +0, not -0
+    for fill in (float("nan"), float("inf"), -float("inf"), torch.finfo(dtype).min):
+        lg[T // 2:] = fill
+        lg[T - 1, : E // 2] = 1.0
+        gw[T // 2:] = fill
+        ids = ops.route_scored(lg, k, scoring=scoring, renorm=renorm, live=live)[0]
+        assert torch.equal(ids, clean[0])
+        got = ops.route_scored_backward(lg, ids, gw, scoring=scoring, renorm=renorm)
+        assert torch.equal(got.view(bits_of), want.view(bits_of))
