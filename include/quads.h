@@ -441,7 +441,8 @@ qd_status moe_route_scored_permute(const void *logits, int32_t dtype, int64_t ld
  *   softmax, renorm:  dl_j = q_j (g_j - sum_i g_i q_i)             at the chosen
  *   softmax:          dl_e = s_e (g_e - sum_i g_i s_i)             at every expert
  * and 0 elsewhere (g_e is 0 for an expert not chosen).  float64, rounded once; of one
- * chosen expert that is renormalised (k = 1) exactly 0.
+ * chosen expert that is renormalised (k = 1) exactly 0.  A token whose weights are NaN
+ * for its logits has NaN wherever these formulas hold one.
  *   topk_ids    : from moe_route_scored_permute; a slot with -1 has no gradient, and a
  *                 token of nothing else gets +0 whatever its logits hold.
  *   grad_w      : f32 [T][k].

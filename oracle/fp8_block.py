@@ -178,7 +178,8 @@ def chosen_weights(logits, ids, scoring, renorm, scale):
 
 def route_backward(logits, ids, grad_w, scoring="softmax", renorm=True, scale=1.0):
     """The gradient of the logits, row by row through the Jacobian of the weights
-    (float64); rows of ids that are -1 have none."""
+    (float64); rows of ids that are -1 have none.  Where the weights depend on the chosen
+    logits alone, the other experts' gradients are 0, beside NaN ones too."""
     x = np.asarray(logits, np.float64)
     T, E = x.shape
     out = np.zeros((T, E))
@@ -192,6 +193,8 @@ def route_backward(logits, ids, grad_w, scoring="softmax", renorm=True, scale=1.
             n = v.sum()
             J = (np.eye(len(v)) / n - np.outer(v, np.ones(len(v))) / n ** 2) @ J if n else 0 * J
         out[t] = float(np.float32(scale)) * np.asarray(grad_w[t], np.float64) @ J
+        if renorm or scoring == "sigmoid":
+            out[t, np.setdiff1d(np.arange(E), ids[t])] = 0.0
     return out
 
 

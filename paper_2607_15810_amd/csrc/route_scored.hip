@@ -301,17 +301,25 @@ __global__ __launch_bounds__(256) void score_grad_kernel(ScoreGradArgs p) {
     for (int e = lane; e < E; e += 64) rs_store<L>(p.grad, t * p.ldg + e, 0.0);
     return;
   }
-  const bool full = p.scoring == QD_SCORE_SOFTMAX && !p.renorm;
+  const bool softmax = p.scoring == QD_SCORE_SOFTMAX, full = softmax && !p.renorm;
   double d = 0.0;                 // this lane's chosen expert's gradient
   double dot = 0.0, z = 1.0;
   float m = 0.0f;
   float x[PER];
-  if (full) {
+  bool broken = false;            // softmax: a NaN or +inf logit leaves no score a number
+  if (softmax) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int e = lane + 64 * j;
       x[j] = e < E ? rs_load<L>(p.logits, t * p.ld + e) : -INFINITY;
+      broken |= !(x[j] < INFINITY);
     }
+    broken = __ballot(broken) != 0ull;
+  }
+  const double nan = __longlong_as_double(0x7ff8000000000000ll);
+  if (broken) {
+    d = nan;
+  } else if (full) {
     m = x[0];
 #pragma unroll
     for (int j = 1; j < PER; ++j) m = fmaxf(m, x[j]);
@@ -324,7 +332,7 @@ __global__ __launch_bounds__(256) void score_grad_kernel(ScoreGradArgs p) {
     const double s = on && m != -INFINITY ? exp((double)xs - (double)m) / z : 0.0;
     dot = rs_wave_sum(s * g);
     d = s * (g - dot);
-  } else if (p.scoring == QD_SCORE_SOFTMAX) {
+  } else if (softmax) {
     const float top = wave_max(on ? xs : -INFINITY);
     const double s = on && top != -INFINITY ? exp((double)xs - (double)top) : 0.0;
     const double n = rs_wave_sum(s);
@@ -347,7 +355,8 @@ __global__ __launch_bounds__(256) void score_grad_kernel(ScoreGradArgs p) {
   for (int j = 0; j < PER; ++j) {
     const int e = lane + 64 * j;
     double v = 0.0;
-    if (full && m != -INFINITY) v = -exp((double)x[j] - (double)m) / z * dot;
+    if (full && broken) v = nan;
+    else if (full && m != -INFINITY) v = -exp((double)x[j] - (double)m) / z * dot;
     for (int q = 0; q < k; ++q) {
       const int eq = __builtin_amdgcn_readlane(id, q);
       const double dq = rs_lane(d, q);

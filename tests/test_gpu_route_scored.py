@@ -301,3 +301,39 @@ def test_gradient_of_dead_tokens_over_stale_logits_is_zero(T, E, dtype, scoring,
         assert torch.equal(ids, clean[0])
         got = ops.route_scored_backward(lg, ids, gw, scoring=scoring, renorm=renorm)
         assert torch.equal(got.view(bits_of), want.view(bits_of))
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,E,k", [(12, 24, 1), (16, 128, 4), (12, 384, 8)])
+def test_gradient_where_the_weights_are_nan(T, E, k, dtype, scoring, renorm):
+    """NaN at the chosen experts (softmax without renormalisation: at every one) of a token
+    whose weights are NaN, zeros at the others, and every other token as it was."""
+    rng = np.random.default_rng(E)
+    x = torch.from_numpy(rng.standard_normal((T, E)).astype(np.float32)).to(dtype).float().numpy()
+    gw = rng.standard_normal((T, k)).astype(np.float32)
+    back = lambda ids, lg: np_of(ops.route_scored_backward(
+        lg, ids, torch.from_numpy(gw).to(DEV), scoring=scoring, renorm=renorm).float())
+    lg = torch.from_numpy(x).to(DEV).to(dtype)
+    clean = back(ops.route_scored(lg, k, scoring=scoring, renorm=renorm)[0], lg)
+    x[1, x[1].argmin()] = np.nan                   # not chosen
+    x[3, :] = np.nan
+    x[4, 5] = np.inf
+    x[5] = -np.inf
+    x[5, 2] = np.nan
+    x[6, x[6].argmax()] = np.nan
+    lg = torch.from_numpy(x).to(DEV).to(dtype)
+    ids = ops.route_scored(lg, k, scoring=scoring, renorm=renorm)[0]
+    got = back(ids, lg)
+    with np.errstate(invalid="ignore"):
+        want = OB.route_backward(x, np_of(ids), gw, scoring, renorm)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    if scoring == "softmax":
+        assert np.isnan(got[[1, 3, 4, 5, 6]]).sum(1).tolist() == [k if renorm else E] * 5
+    same = [0, 2] + list(range(7, T))
+    assert np.array_equal(got[same], clean[same])
+    half = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8 * (1 + 2.0 ** -15)
+    fine = ~np.isnan(want)
+    err = np.abs(got.astype(np.float64) - want)[fine]
+    assert (err <= half * np.abs(want[fine]) * 1.001 + 2.0 ** -38).all()
