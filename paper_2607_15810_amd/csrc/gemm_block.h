@@ -7,6 +7,8 @@
 namespace qdb {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 struct BlkArgs {
   const uint8_t *a;            // [a_rows][K]
@@ -25,14 +27,19 @@ struct BlkArgs {
 
 static __device__ const uint4 bk_zero = {0, 0, 0, 0};
 
-__device__ __forceinline__ f16x2 dec2(uint32_t w, bool hi) {
-  return hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true)
-            : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false);
+// eight codes (two words) times the power of two of sc, exact in bf16
+__device__ __forceinline__ bf16x8 dec8b(uint32_t lo, uint32_t hi, float sc) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, sc, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, sc, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, sc, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, sc, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// eight codes (two words) to f16, exact
-__device__ __forceinline__ f16x8 dec8(uint32_t lo, uint32_t hi) {
-  const f16x2 a = dec2(lo, false), b = dec2(lo, true), c = dec2(hi, false), d = dec2(hi, true);
-  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+// the mantissa of a scale with its sign, of size in [1, 2); NaN of a scale that is not finite
+__device__ __forceinline__ float bk_mant(float v) {
+  const uint32_t b = __float_as_uint(v);
+  const float m = __uint_as_float((b & 0x807FFFFFu) | 0x3F800000u);
+  return (b & 0x7F800000u) == 0x7F800000u ? __uint_as_float(0x7FC00000u) : m;
 }
 __device__ __forceinline__ float bk_swiglu(float g, float u) {
   const float ex = __builtin_amdgcn_exp2f(-g * 1.4426950408889634f);

@@ -52,24 +52,6 @@ using namespace qdb;
 using namespace qdl;
 using namespace qdp;
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-// eight codes (two words) times the power of two of sc, exact in bf16
-__device__ __forceinline__ bf16x8 dec8b(uint32_t lo, uint32_t hi, float sc) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, sc, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, sc, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, sc, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, sc, true);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-// the mantissa of a scale with its sign, of size in [1, 2); NaN of a scale that is not finite
-__device__ __forceinline__ float bk_mant(float v) {
-  const uint32_t b = __float_as_uint(v);
-  const float m = __uint_as_float((b & 0x807FFFFFu) | 0x3F800000u);
-  return (b & 0x7F800000u) == 0x7F800000u ? __uint_as_float(0x7FC00000u) : m;
-}
-
 template <int MF>
 struct BkCfg {
   static constexpr int M = 64 * MF;

@@ -5,7 +5,7 @@
 // Here a workgroup takes 32 weight rows of one expert and up to 8 or 32 of its rows, and
 // its four waves split K: wave w takes the blocks w, w + 4, .. of 128, each through a ring of
 // its own (weights, rows and scales, direct global->LDS loads counted by hand, no barrier),
-// with the operands decoded to f16, exactly.  The waves' float32 sums are joined in LDS in
+// with the operands decoded to bf16, exactly.  The waves' float32 sums are joined in LDS in
 // wave order, so that a row's bits are the same in tiles of 8 and of 32.  With the quantising
 // epilogue h goes to workspace in float32 and a second launch quantises it: a block of 128 of
 // h spans eight workgroups.  The layer's down product of one token or two takes that h
@@ -141,16 +141,19 @@ __global__ __launch_bounds__(256) void gemm_block_few_kernel(BlkArgs p, int nfr,
       ca[k] = *reinterpret_cast<const uint4 *>(sl + C::A + ar * 128 + ((pc ^ sa) << 4));
     }
     const float *ss = reinterpret_cast<const float *>(sl + C::S);
-    const float s0 = ss[ar] * ss[ROWS], s1 = ss[ar] * ss[ROWS + 1];
+    // the scales' exponents go into the operands, the product of their mantissas stays: no
+    // product of two scales leaves float32's range where the result does not
+    const float as = ss[ar], w0 = ss[ROWS], w1 = ss[ROWS + 1], wr = r & 16 ? w1 : w0;
+    const float s0 = bk_mant(as) * bk_mant(w0), s1 = bk_mant(as) * bk_mant(w1);
     f32x16 part;
 #pragma unroll
     for (int q = 0; q < 16; ++q) part[q] = 0.0f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      part = __builtin_amdgcn_mfma_f32_32x32x16_f16(dec8(cw[k].x, cw[k].y), dec8(ca[k].x, ca[k].y),
-                                                    part, 0, 0, 0);
-      part = __builtin_amdgcn_mfma_f32_32x32x16_f16(dec8(cw[k].z, cw[k].w), dec8(ca[k].z, ca[k].w),
-                                                    part, 0, 0, 0);
+      part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dec8b(cw[k].x, cw[k].y, wr),
+                                                     dec8b(ca[k].x, ca[k].y, as), part, 0, 0, 0);
+      part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dec8b(cw[k].z, cw[k].w, wr),
+                                                     dec8b(ca[k].z, ca[k].w, as), part, 0, 0, 0);
     }
     // the slot is in registers
     wait_lds();

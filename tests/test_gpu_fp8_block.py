@@ -285,6 +285,58 @@ def test_scales_of_the_largest_and_smallest_sizes(rows):
 
 
 @pytest.mark.parametrize("rows", [3, 200, 6000])
+@pytest.mark.parametrize("ea,ew", [(-73, -73), (-109, -37), (-37, -109)])
+def test_products_of_small_scales(rows, ea, ew):
+    """Scales whose product is far below float32's normal numbers under sums that lift the
+    results to them: bf16's steps are 2^-133 from 2^-126 down, and float32 sums that are
+    subnormal round by 2^-150 a product more (K = 528: less than 2^-140 together)."""
+    rng = np.random.default_rng(rows)
+    N, K = 192, 528
+    a, sa, w, sw, _, offs, _ = make(rng, [rows], N, K, gather=False)
+    sa = rng.uniform(1, 2, sa.shape).astype(np.float32) * np.float32(2.0 ** ea)
+    sw = rng.uniform(1, 2, sw.shape).astype(np.float32) * np.float32(2.0 ** ew)
+    ref, mag = refs(a, sa, w, sw, None, offs)
+    assert (np.abs(ref) > 2.0 ** -127).mean() > 0.25
+    y = ops.fp8_block_grouped_gemm(up(a), up(sa), up(w), up(sw), rows)
+    err = np.abs(np_of(y.float()).astype(np.float64) - ref)
+    bound = HALF * np.abs(ref) + FLOOR * mag * (1 + HALF) + 2.0 ** -134 + 2.0 ** -140
+    assert (err <= bound).all(), f"{(err > bound).sum()} of {err.size}, worst {(err / bound).max()}"
+
+
+@pytest.mark.parametrize("rows", [3, 200, 6000])
+def test_products_of_large_scales(rows):
+    """Two scales whose product no float32 holds: over products that are all zero they add
+    nothing, over small ones what those make."""
+    rng = np.random.default_rng(rows)
+    N, K = 192, 528
+    a, sa, w, sw, _, offs, _ = make(rng, [rows], N, K, gather=False)
+    a[:, 128:256] &= 0x80                          # zeros of either sign
+    a[:, 256:384] = 0x01 | (a[:, 256:384] & 0x80)  # 2^-9, against weights of 2^-9
+    w[:, :, 256:384] = 0x01 | (w[:, :, 256:384] & 0x80)
+    ref, mag = refs(a, sa, w, sw, None, offs)
+    sa[1], sw[:, :, 1] = np.float32(2.0 ** 70), np.float32(1.5 * 2.0 ** 75)
+    y = ops.fp8_block_grouped_gemm(up(a), up(sa), up(w), up(sw), rows)
+    check_bf16(y, ref, mag)
+    sa[2], sw[:, :, 2] = np.float32(1.5 * 2.0 ** 66), np.float32(1.25 * 2.0 ** 66)
+    ref, mag = refs(a, sa, w, sw, None, offs)
+    check_bf16(ops.fp8_block_grouped_gemm(up(a), up(sa), up(w), up(sw), rows), ref, mag)
+
+
+@pytest.mark.parametrize("rows", [3, 200, 6000])
+def test_an_infinite_scale_makes_nan(rows):
+    rng = np.random.default_rng(rows)
+    N, K = 256, 400
+    a, sa, w, sw, _, offs, _ = make(rng, [rows], N, K, gather=False)
+    for bad in (float("inf"), -float("inf"), float("nan")):
+        s, v = up(sa), up(sw)
+        s[2, 0] = bad
+        assert torch.isnan(ops.fp8_block_grouped_gemm(up(a), s, up(w), v, rows)[0]).all()
+        s, v[0, 1, 2] = up(sa), bad
+        y = ops.fp8_block_grouped_gemm(up(a), s, up(w), v, rows)
+        assert torch.isnan(y[:, 128:]).all() and torch.isfinite(y[:, :128]).all()
+
+
+@pytest.mark.parametrize("rows", [3, 200, 6000])
 def test_scales_of_zero_and_not_finite(rows):
     rng = np.random.default_rng(rows)
     N, K = 256, 400
