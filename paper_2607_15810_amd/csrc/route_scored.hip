@@ -272,9 +272,15 @@ template <>
 __device__ __forceinline__ void rs_store<float>(void *p, int64_t i, double v) {
   static_cast<float *>(p)[i] = (float)v;
 }
+// one rounding: by way of a float32 that is rounded to odd (the even neighbour of a value in
+// between would hide from the second rounding on which side of a tie it lies)
 template <>
 __device__ __forceinline__ void rs_store<uint16_t>(void *p, int64_t i, double v) {
-  static_cast<__bf16 *>(p)[i] = (__bf16)(float)v;
+  const float f = (float)v;
+  const double a = fabs((double)f), b = fabs(v);
+  uint32_t bits = __float_as_uint(f);
+  if ((a < b || a > b) && !(bits & 1u)) bits += a < b ? 1u : 0xFFFFFFFFu;
+  static_cast<__bf16 *>(p)[i] = (__bf16)__uint_as_float(bits);
 }
 
 // One wavefront per token; lane j < k holds chosen expert j.

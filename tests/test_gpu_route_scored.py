@@ -337,3 +337,29 @@ def test_gradient_where_the_weights_are_nan(T, E, k, dtype, scoring, renorm):
     fine = ~np.isnan(want)
     err = np.abs(got.astype(np.float64) - want)[fine]
     assert (err <= half * np.abs(want[fine]) * 1.001 + 2.0 ** -38).all()
+
+
+def test_bf16_gradient_is_rounded_once():
+    """Sigmoid at 0: the gradient is scale * grad_w / 4, exact in float64.  Products next to the
+    middle of two bf16 numbers, nearer than float32 can tell."""
+    T, E = 512, 8
+    scale = np.float32(1.6369615793)
+    m = np.arange(T * E).reshape(T, E)
+    middle = (1 + (2 * (m % 128) + 1) * 2.0 ** -8) * 2.0 ** (m // 128 - 16)
+    gw = (middle / np.float64(scale)).astype(np.float32) * np.where(m % 3, 1, -1).astype(np.float32)
+    v = np.float64(scale) * gw.astype(np.float64) / 4
+    step = 2.0 ** (np.floor(np.log2(np.abs(v))) - 7)
+    want = np.round(v / step) * step               # to even, one rounding
+    by_float = (v.astype(np.float32) / step)
+    assert (np.round(by_float) * step != want).sum() > 200
+    ids = torch.arange(E, dtype=torch.int32, device=DEV).repeat(T, 1)
+    got = ops.route_scored_backward(torch.zeros((T, E), dtype=torch.bfloat16, device=DEV), ids,
+                                    torch.from_numpy(gw).to(DEV), scoring="sigmoid", renorm=False,
+                                    scale=float(scale))
+    assert np.array_equal(np_of(got.float()).astype(np.float64), want)
+    # beyond bf16's largest number, and below its smallest
+    big = torch.tensor([[3.39e38, -3.3961776e38, 3.4028235e38, 1e-45]], device=DEV)
+    got = ops.route_scored_backward(torch.zeros((1, 4), dtype=torch.bfloat16, device=DEV),
+                                    ids[:1, :4].contiguous(), big, scoring="sigmoid", renorm=False,
+                                    scale=4.0)
+    assert torch.equal(got, big.to(torch.bfloat16))
