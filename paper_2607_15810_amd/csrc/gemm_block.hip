@@ -15,8 +15,10 @@
 // block's u and are multiplied by u_before / u once a block, one multiplication per element,
 // and once by u at the end.  (Partial sums of a block folded into a total by a
 // multiply-add cost the same instruction and a second set of accumulators, and those kept
-// tiles at 128 rows: 4096^3 137 -> 121 us.)  The unit's reciprocal is the hardware's: the
-// unit kept is the one multiplied by, off by less than 2^-22 a block.
+// tiles at 128 rows: 4096^3 137 -> 121 us.)  The quotient of the units is corrected to its
+// rounding (two instructions a fragment and block, at most 1% of a call): blocks of one unit
+// are not rescaled at all, where the hardware's reciprocal alone made every block shrink what
+// was summed by up to 2^-22, always to the same side (K = 7168: 2^-19.6 of a half's sum).
 //
 // The weights are the instruction's first operand, so a lane holds one activation row: its
 // row scale is one register, and the columns of a row leave a lane together.
@@ -328,8 +330,9 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
           const float ma = bk_mant(v.r[i]);
 #pragma unroll
           for (int g = 0; g < NS; ++g) {
-            const float u = ma * bk_mant(v.w[g]);
-            rho[g] = unit[i][g] * __builtin_amdgcn_rcpf(u);
+            const float u = ma * bk_mant(v.w[g]), rc = __builtin_amdgcn_rcpf(u);
+            const float q = unit[i][g] * rc;       // and its error: the quotient rounded, 1 of equal units
+            rho[g] = __builtin_fmaf(__builtin_fmaf(-q, u, unit[i][g]), rc, q);
             unit[i][g] = u;
           }
         }

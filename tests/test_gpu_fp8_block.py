@@ -398,6 +398,54 @@ def test_offsets_past_32_bits():
     assert torch.equal(codes[-40:], c) and torch.equal(scales[:, -40:], s)
 
 
+# (the first two on the large kernel, the last on that of few rows)
+@pytest.mark.parametrize("rows,N,K", [(1400, 2560, 7168), (1400, 2560, 2816), (9, 256, 7168)])
+def test_long_sums_do_not_drift(rows, N, K):
+    """The second half of K takes off what the first has summed: 0 to the exact sum, so what is
+    left is the rounding.  Codes of 1/4 to 4: the products of a half are multiples of 2^-10
+    whose sums stay below 2^14, so the float32 sums of one unit are exact.  The large kernel's
+    are then 0 where all blocks have the same scales.  Of others, a block is rescaled K / 128
+    times at most by a quotient and a product, 2^-24 each, its unit is a product rounded
+    once: (K / 128 + 1) 2^-23 of the sum of |products|.  The few-rows kernel folds a block with
+    two roundings of the total, and joins four: as many."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(K)
+    half = lambda *n: torch.randint(0x28, 0x49, n, dtype=torch.uint8, generator=g, device=DEV)
+    a, w = half(rows, K // 2), half(1, N, K // 2)
+    a, w = torch.cat([a, a ^ 0x80], 1), torch.cat([w, w], 2)
+    blocks, nb = K // 256, N // 128
+    v = lambda c: c.view(torch.float8_e4m3fn).float()
+    assert float((v(a[:, :K // 2]) @ v(w[0, :, :K // 2]).t()).max()) < 2 ** 14
+    for ma, mw in ((1.3, 1.7), (1.0, 1.37), (1.9, 1.1), (1.5, 1.25), (1.77, 1.61)):
+        sa = torch.full((2 * blocks, rows), ma, device=DEV)
+        sw = torch.full((1, nb, 2 * blocks), mw, device=DEV)
+        y = ops.fp8_block_grouped_gemm(a, sa, w, sw, rows)
+        if rows > 9:
+            assert not y.any()
+    sa = torch.rand((blocks, rows), generator=g, device=DEV) + 0.5
+    sw = torch.rand((1, nb, blocks), generator=g, device=DEV) + 0.5
+    sa, sw = torch.cat([sa, sa]), torch.cat([sw, sw], 2)
+    y = ops.fp8_block_grouped_gemm(a, sa, w, sw, rows)
+    wide = lambda s, n: s.repeat_interleave(128, 0)[:n].double()
+    mag = (v(a).abs().double() * wide(sa, K).t()) @ (
+        v(w[0]).double() * wide(sw[0].t().contiguous(), K).t().repeat_interleave(128, 0)[:N]).t()
+    assert (y.double().abs() <= mag * (K / 128 + 1) * 2.0 ** -23 * (1 + HALF)).all()
+
+
+@pytest.mark.parametrize("counts,N,K", [([700, 650], 2560, 7168), ([1300], 2560, 20480)])
+def test_long_k_on_the_large_kernel(counts, N, K):
+    """Against the oracle: half a bf16 step, (K / 128 + 1) 2^-23 of rescaling and the rounding of
+    K / 4 steps of the sum so far, 0.63 sqrt(K) 2^-23 of the sum of |products|."""
+    rng = np.random.default_rng(K)
+    a, sa, w, sw, tok, offs, rows = make(rng, counts, N, K, a_rows=60)
+    assert Q.lib().moe_fp8_block_grouped_gemm_workspace(rows, N, K, len(counts), Q.QD_EPI_SWIGLU_FP8) == 0
+    ref, mag = refs(a, sa, w, sw, tok, offs)
+    y = ops.fp8_block_grouped_gemm(up(a), up(sa), up(w), up(sw), rows, up(tok), up(offs))
+    err = np.abs(np_of(y.float()).astype(np.float64) - ref)
+    floor = (K / 128 + 1 + 0.63 * K ** 0.5) * 2.0 ** -23
+    assert (err <= HALF * np.abs(ref) + floor * mag * (1 + HALF)).all()
+
+
 def random_codes(E, N, K, rows, seed):
     g = torch.Generator(device=DEV)
     g.manual_seed(seed)
