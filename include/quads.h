@@ -423,7 +423,8 @@ qd_status qd_fp8_moe_layer_forward(const void *x, const float *logits, int64_t T
  *   ws      : at least moe_route_scored_workspace(T, E, k) bytes (0 up to 256 tokens;
  *             NULL is allowed there).
  *   1 <= k <= 32, k <= top_groups * (E / groups), E <= 1024, groups <= 64,
- *   E % groups == 0, scale finite.
+ *   E % groups == 0, scale finite; at most 2^26 - 4 tokens (QD_ERR_UNSUPPORTED), as in
+ *   the gradient.
  * ------------------------------------------------------------------- */
 size_t    moe_route_scored_workspace(int64_t T, int32_t E, int32_t k);
 qd_status moe_route_scored_permute(const void *logits, int32_t dtype, int64_t ld, int64_t T,
@@ -476,6 +477,7 @@ qd_status moe_route_scored_backward(const void *logits, int32_t dtype, int64_t l
  *              and f32 [groups][ceil(cols / 128)][ceil(rows / 128)], written in the
  *              same pass (rows % 16 == 0): with it moe_fp8_block_grouped_gemm
  *              gives the gradient of its activations, dx = dy w.
+ * From 2^28 rows of activations or 2^24 blocks of weights on QD_ERR_UNSUPPORTED.
  * ------------------------------------------------------------------- */
 qd_status fp8_block_quantize_act(const void *x, int32_t dtype, int64_t rows, int64_t cols,
                                  int64_t ld, uint8_t *codes, float *scales, void *stream);

@@ -261,6 +261,12 @@ inline hipStream_t S(void *s) { return reinterpret_cast<hipStream_t>(s); }
 
 inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 
+// Whether a grid of `blocks` workgroups can be launched: one dimension holds fewer than 2^32
+// threads.
+inline bool grid_fits(int64_t blocks, int threads) {
+  return blocks <= 0xffffffffLL / threads && blocks <= 0x7fffffffLL;
+}
+
 qd_status check_nvfp4(const qd_nvfp4 *t, int64_t groups, int64_t rows, int64_t cols);
 
 }  // namespace qdh

@@ -125,7 +125,7 @@ extern "C" qd_status fp8_block_quantize_act(const void *x, int32_t dtype, int64_
   if (!x || !codes || !scales) return QD_ERR_NULL;
   if (!qdh::aligned16(x) || !qdh::aligned16(codes) || !qdh::aligned16(scales)) return QD_ERR_ALIGN;
   const int64_t gx = (rows - 1) / 16 + 1, gy = (cols - 1) / (4 * FB) + 1;
-  if (gx > 0x7fffffffLL || gy > 65535) return QD_ERR_UNSUPPORTED;
+  if (!qdh::grid_fits(gx, 256) || gy > 65535) return QD_ERR_UNSUPPORTED;
   if (qdh::fault_injected()) return QD_ERR_HIP;
   hipStream_t s = qdh::S(stream);
   const dim3 grid((unsigned)gx, (unsigned)gy), block(256);
@@ -152,7 +152,9 @@ extern "C" qd_status fp8_block_quantize_weight(const void *w, int32_t dtype, int
       !qdh::aligned16(codes_t) || !qdh::aligned16(scales_t))
     return QD_ERR_ALIGN;
   const int64_t nnb = (rows - 1) / FB + 1, nkb = (cols - 1) / FB + 1;
-  if (nnb > 0x7fffffffLL / nkb || groups > 0x7fffffffLL / (nnb * nkb)) return QD_ERR_UNSUPPORTED;
+  if (nnb > 0x7fffffffLL / nkb || groups > 0x7fffffffLL / (nnb * nkb) ||
+      !qdh::grid_fits(groups * nnb * nkb, 256))
+    return QD_ERR_UNSUPPORTED;
   if (qdh::fault_injected()) return QD_ERR_HIP;
   if (dtype == QD_DTYPE_BF16)
     launch_weight<uint16_t>(w, groups, rows, cols, codes, scales, codes_t, scales_t, qdh::S(stream));

@@ -413,9 +413,9 @@ qd_status route_scored(
       !qdh::aligned16(topk_w) || !qdh::aligned16(expert_offsets) || !qdh::aligned16(row_token) ||
       !qdh::aligned16(inv_row) || !qdh::aligned16(ws))
     return QD_ERR_ALIGN;   // (NULL is aligned)
-  if (qdh::fault_injected()) return QD_ERR_HIP;
   hipStream_t s = qdh::S(stream);
   if (T == 0) {
+    if (qdh::fault_injected()) return QD_ERR_HIP;
     qdi::launch_fill_i32(expert_offsets, E + 1, 0, s);
     return qdh::check_launch();
   }
@@ -430,7 +430,8 @@ qd_status route_scored(
   ActBeside act{static_cast<const uint16_t *>(x), T, cols, x_codes, x_scales, (int)groups_of,
                 (int)((T + arows - 1) / arows)};
   const int64_t acts = x ? act.nb * ((cols + 4 * qdb::FB - 1) / (4 * qdb::FB)) : 0;
-  if (groups_of + acts > 0x7fffffffLL) return QD_ERR_UNSUPPORTED;
+  if (!qdh::grid_fits(groups_of + acts, one ? 1024 : 256)) return QD_ERR_UNSUPPORTED;
+  if (qdh::fault_injected()) return QD_ERR_HIP;
   const dim3 grid((unsigned)(groups_of + acts));
   if (one) {
     rs_by_width(sl.per, [&](auto w) {
@@ -488,6 +489,7 @@ extern "C" qd_status moe_route_scored_backward(const void *logits, int32_t dtype
   if (!qdh::aligned16(logits) || !qdh::aligned16(topk_ids) || !qdh::aligned16(grad_w) ||
       !qdh::aligned16(grad_logits))
     return QD_ERR_ALIGN;
+  if (!qdh::grid_fits((T + 3) / 4, 256)) return QD_ERR_UNSUPPORTED;
   if (qdh::fault_injected()) return QD_ERR_HIP;
   hipStream_t s = qdh::S(stream);
   ScoreGradArgs p{logits, ld, T, E, k, scoring, renorm, scale, topk_ids, grad_w, grad_logits, ld_grad};

@@ -138,3 +138,22 @@ def test_injected_launch_failure(monkeypatch):
     monkeypatch.setenv("QD_FAULT_INJECT", "launch")
     assert route() == Q.QD_ERR_HIP
     assert gemm() == Q.QD_ERR_HIP
+
+
+def test_more_threads_than_a_launch_holds(monkeypatch):
+    """One dimension of a launch has fewer than 2^32 threads: refused here, not by the launch."""
+    monkeypatch.setenv("QD_FAULT_INJECT", "launch")
+    huge = 1 << 45
+    assert route(T=(1 << 26) - 4, n=huge) == Q.QD_ERR_HIP
+    assert route(T=1 << 26, n=huge) == Q.QD_ERR_UNSUPPORTED
+    back = lambda T: Q.raw("moe_route_scored_backward", P, 0, 16, T, 16, 2, 1, 1, 1.0, P, P, P, 16, None)
+    assert back((1 << 26) - 4) == Q.QD_ERR_HIP and back(1 << 26) == Q.QD_ERR_UNSUPPORTED
+    act = lambda rows: Q.raw("fp8_block_quantize_act", P, 0, rows, 16, 16, P, P, None)
+    assert act((1 << 28) - 16) == Q.QD_ERR_HIP and act(1 << 28) == Q.QD_ERR_UNSUPPORTED
+    bank = lambda groups: Q.raw("fp8_block_quantize_weight", P, 0, groups, 16, 16, P, P, None, None, None)
+    assert bank((1 << 24) - 1) == Q.QD_ERR_HIP and bank(1 << 24) == Q.QD_ERR_UNSUPPORTED
+    # the layer refuses before its first launch
+    monkeypatch.delenv("QD_FAULT_INJECT")
+    n = Q.lib().qd_fp8_block_moe_layer_workspace(1 << 26, 16, 16, 2, 32)
+    assert Q.raw("qd_fp8_block_moe_layer_forward", P, P, 1 << 26, 16, 16, 2, 32, 0, None, 1, 1, 1, 1,
+                 1.0, None, P, P, P, P, P, P, n, None) == Q.QD_ERR_UNSUPPORTED
