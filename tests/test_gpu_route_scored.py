@@ -363,3 +363,25 @@ def test_bf16_gradient_is_rounded_once():
                                     ids[:1, :4].contiguous(), big, scoring="sigmoid", renorm=False,
                                     scale=4.0)
     assert torch.equal(got, big.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,E,k", [(20, 200, 8), (9, 256, 32), (14, 257, 8), (11, 384, 6),
+                                   (9, 512, 8), (10, 513, 1), (9, 1024, 32)])
+def test_gradient_of_many_experts(T, E, k, dtype, scoring, renorm):
+    """Every width of the kernel, rows E + 5 apart, against the oracle."""
+    rng = np.random.default_rng(T + E)
+    wide = torch.from_numpy((2 * rng.standard_normal((T, E + 5))).astype(np.float32)).to(DEV).to(dtype)
+    lg = wide[:, :E]
+    live = rng.random(T) < 0.8
+    ids = ops.route_scored(lg, k, scoring=scoring, renorm=renorm, scale=2.5,
+                           live=torch.from_numpy(live).to(DEV))[0]
+    gw = rng.standard_normal((T, k)).astype(np.float32)
+    got = np_of(ops.route_scored_backward(lg, ids, torch.from_numpy(gw).to(DEV), scoring=scoring,
+                                          renorm=renorm, scale=2.5).float()).astype(np.float64)
+    want = OB.route_backward(np_of(lg.float()), np_of(ids), gw, scoring, renorm, 2.5)
+    half = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8
+    assert (np.abs(got - want) <= half * np.abs(want) * 1.001 + 2.5 * 2.0 ** -38).all()
+    assert not got[~live].any()
