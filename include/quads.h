@@ -491,7 +491,7 @@ qd_status fp8_block_quantize_weight(const void *w, int32_t dtype, int64_t groups
  *   v[r][n] = sum_b a_scales[b][src(r)] w_scales[e][n / 128][b]
  *                   sum_{k in b} a[src(r)][k] w[e][n][k]
  * (products exact, f32 sums; on the 16-bit MFMAs, since the FP8 ones sum at less).
- * Scales are finite numbers below 2^118 in size; one that is not finite makes its rows
+ * Scales are finite numbers below 2^120 in size; one that is not finite makes its rows
  * or columns NaN, and one below 2^-126 counts as a value near 2^-127.
  *   a_codes, a_scales : u8 [a_rows][K], f32 [ceil(K / 128)][a_rows];  row_token (values
  *                     in [0, a_rows) below expert_offsets[E]) and expert_offsets as in

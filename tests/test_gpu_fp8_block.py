@@ -617,3 +617,47 @@ def test_combine_skips_slots_without_a_row():
     w = torch.tensor([[0.5, 1.0], [1.0, 1.0], [1.0, 2.0]], device=DEV)
     y = ops.unpermute_combine(z, inv, w)
     assert (y[0] == 1.0).all() and (y[1] == 0.0).all() and (y[2] == 7.0).all()
+
+
+@pytest.mark.parametrize("rows", [3, 200, 6000])
+def test_products_of_the_largest_numbers(rows):
+    """What the quantisers make of the types' largest numbers (scales to 2^119.2) is multiplied
+    like any other, on either side."""
+    rng = np.random.default_rng(rows)
+    N, K = 192, 528
+    top = float(torch.finfo(torch.bfloat16).max)
+    for side in range(2):
+        x = rng.standard_normal((rows, K)).astype(np.float32)
+        w = rng.standard_normal((1, N, K)).astype(np.float32)
+        big, small = (x, w) if side == 0 else (w, x)
+        big /= np.abs(big).max()
+        big[..., ::3] = np.sign(big[..., ::3])
+        small *= np.float32(1e-30)
+        t = torch.from_numpy(big).to(DEV) * top
+        a = ops.fp8_block_quantize_act(t.to(torch.bfloat16) if side == 0 else up(small))
+        b = ops.fp8_block_quantize_weight(t.to(torch.bfloat16) if side == 1 else up(small))
+        assert float((a if side == 0 else b)[1].max()) > 2.0 ** 119
+        ref, mag = refs(*map(np_of, a), *map(np_of, b), None, np.array([0, rows]))
+        check_bf16(ops.fp8_block_grouped_gemm(*a, *b, rows), ref, mag)
+
+
+@pytest.mark.parametrize("counts", [[5, 2], [40, 30], [4000, 3000]])
+def test_nan_and_overflow_through_the_epilogues(counts):
+    """A NaN row of h is NaN codes under a scale of 1; an h past float32 makes its block NaN
+    (an infinite scale); the other rows keep their bits."""
+    rng = np.random.default_rng(14)
+    N, K = 512, 272
+    a, sa, w, sw, tok, offs, rows = make(rng, counts, N, K, gather=False)
+    args = [up(a), up(sa), up(w), up(sw), rows, None, up(offs)]
+    run = lambda e: ops.fp8_block_grouped_gemm(*args, epilogue=e)
+    y, (c, s) = run("swiglu"), run("swiglu_quant")
+    args[0][4, 100] = 0x7F
+    args[1][:, 1] = 2.0 ** 110                     # g u of about 2^230
+    y2, (c2, s2) = run("swiglu"), run("swiglu_quant")
+    keep = [r for r in range(rows) if r not in (1, 4)]
+    assert torch.equal(y2[keep], y[keep]) and torch.equal(c2[keep], c[keep])
+    assert torch.equal(s2[:, keep], s[:, keep])
+    assert torch.isnan(y2[4]).all() and ((c2[4] & 0x7F) == 0x7F).all() and (s2[:, 4] == 1).all()
+    assert torch.isinf(y2[1]).any() and torch.isinf(s2[:, 1]).all()
+    v = c2[1].view(torch.float8_e4m3fn).float() * s2[:, 1].repeat_interleave(128)
+    assert torch.isnan(v).all()
