@@ -402,9 +402,9 @@ qd_status qd_fp8_moe_layer_forward(const void *x, const float *logits, int64_t T
  *   the k largest c are chosen, in that order (ties to the lower expert);
  *   weight = scale * s / (sum of s over the chosen) with renorm 1 (0 where
  *   that sum is 0), scale * s with renorm 0.  bias enters the choice only.
- * Scores, sums and comparisons are float64.  Without bias and groups the order is
- * that of the logits; softmax scores are renormalised as a softmax over the
- * chosen logits.
+ * Scores, sums and comparisons are float64 (sigmoids of 37 and more are all 1 there, and
+ * tie).  Without bias and groups the order is that of the logits, saturated or not;
+ * softmax scores are renormalised as a softmax over the chosen logits.
  *   logits  : [T] rows of E elements of dtype (QD_DTYPE_BF16 or QD_DTYPE_F32), ld
  *             elements apart (ld >= E).  -inf is an expert with score 0.  A NaN is
  *             chosen last (a group whose score it enters too), and the experts of a
@@ -441,7 +441,7 @@ qd_status moe_route_scored_permute(const void *logits, int32_t dtype, int64_t ld
  *   sigmoid:          dl_j = g_j s_j (1 - s_j)                     at the chosen
  *   softmax, renorm:  dl_j = q_j (g_j - sum_i g_i q_i)             at the chosen
  *   softmax:          dl_e = s_e (g_e - sum_i g_i s_i)             at every expert
- * and 0 elsewhere (g_e is 0 for an expert not chosen).  float64, rounded once; of one
+ * and 0 elsewhere (g_e is 0 for an expert not chosen).  float64, rounded once to dtype; of one
  * chosen expert that is renormalised (k = 1) exactly 0.  A token whose weights are NaN
  * for its logits has NaN wherever these formulas hold one.
  *   topk_ids    : from moe_route_scored_permute; a slot with -1 has no gradient, and a
@@ -506,6 +506,8 @@ qd_status fp8_block_quantize_weight(const void *w, int32_t dtype, int64_t groups
  *   out_scales      : QD_EPI_SWIGLU_FP8 only (ignored otherwise, NULL allowed).
  *   ws              : moe_fp8_block_grouped_gemm_workspace(...) bytes (up to some hundred
  *                     rows with QD_EPI_SWIGLU_FP8 need some; NULL allowed where it is 0).
+ * A row's result does not depend on the other rows or its place, up to the order of its sums: two
+ * kernels share the calls, by their sizes, and differ in it.
  * K % 16 == 0, E <= 1024; activation codes and one expert's weights below 4 GiB, fewer than
  * 2^30 rows (otherwise QD_ERR_UNSUPPORTED).  Rows from expert_offsets[E] on are left as they were.
  * ------------------------------------------------------------------- */

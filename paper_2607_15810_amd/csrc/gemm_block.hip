@@ -33,9 +33,11 @@
 //    filled by direct global->LDS loads.
 //  * Bound, for hundreds of rows per expert, by the matrix unit and the vector unit beside
 //    it: 7 vector instructions per MFMA (decoding 3 to 4, rescaling 2), the matrix unit
-//    busy 51% of the cycles at 2.1 GHz (4096^3: 1.13 PFLOP/s; an isolated loop of the same
-//    instructions on random operands, which the chip's power limits, reaches 1.5), of
-//    experts 0.73 to 0.8 PFLOP/s (the epilogue, tiles of uneven height, weights from HBM).
+//    busy 50% of the cycles at 2.1 GHz (4096^3: 1.05 to 1.13 PFLOP/s by the box; an isolated
+//    loop of the same instructions on random operands, which the chip's power limits, reaches
+//    1.5).  Of experts 0.73 to 0.8 PFLOP/s, busy 32 to 39%: tiles of uneven height (9 to 10
+//    vector instructions per MFMA), the epilogue, weights from HBM, and a stage's loads, which
+//    all eight waves issue together after the barrier with no MFMA beside them.
 //    For tens of rows by HBM: 5.1 to 5.4 TB/s of weights.
 //  * Calls of a few rows, whose tiles would leave most CUs idle, run on the kernel of
 //    gemm_block_few.hip.
@@ -159,8 +161,8 @@ __global__ __launch_bounds__(PN_THREADS, 2) void gemm_block_kernel(BlkArgs p, Pn
     // Where the tile starts in K.  Rows that lie a multiple of 4 KB apart put a block on a
     // few memory channels, and workgroups that all start at block 0 meet there: each
     // weight-row tile has a place of its own.  (Not each expert too, which would be 1 to 3%
-    // faster still: a row's bits depend on neither the batch, the schedule nor the
-    // expert's number.)  128 experts of 16 rows, N = 1536: K = 4096 187 -> 154 us, K = 4224, from
+    // faster still: within this kernel a row's bits depend on neither the batch, the schedule
+    // nor the expert's number.)  128 experts of 16 rows, N = 1536: K = 4096 187 -> 154 us, K = 4224, from
     // block 0 on, 152; 256 rows, K = 768: 141 from block 0, 147 spread.
     kb = K % 4096 == 0 ? (int)uni((uint32_t)(13 * itl.nt) % (uint32_t)KB) : 0;
     wb = uni_ptr(q->w + (int64_t)itl.e * N * K + kb * FB);

@@ -6,14 +6,15 @@
 // its four waves split K: wave w takes the blocks w, w + 4, .. of 128, each through a ring of
 // its own (weights, rows and scales, direct global->LDS loads counted by hand, no barrier),
 // with the operands decoded to bf16, exactly.  The waves' float32 sums are joined in LDS in
-// wave order, so that a row's bits are the same in tiles of 8 and of 32.  With the quantising
+// wave order, so that a row's bits are the same in tiles of 8 and of 32 (not those of the large
+// kernel, which sums in another order).  With the quantising
 // epilogue h goes to workspace in float32 and a second launch quantises it: a block of 128 of
 // h spans eight workgroups.  The layer's down product of one token or two takes that h
 // instead (HIN) and each wave quantises the blocks it needs, a launch less.
 //
 // Bound by latency: launch, tile search, row indices, the first block, the join (5 to 7 us
 // at one row), and then by workgroups: two on a CU, 6 us a round of 512 at K = 2048.  8 experts
-// of a row, K = 2048, N = 1536: 10 us, 2.5 TB/s of weights.
+// of a row, K = 2048, N = 1536: 10 us, 2.5 TB/s of weights; K = 7168, N = 4096: 50, 4.7 TB/s.
 #include "gemm_block.h"
 #include "lds_dma.h"
 #include "tile_sched.h"
@@ -220,7 +221,10 @@ static double few_tiles(double rows, int E, double h) {
 // (us), fitted to graphs of ten calls (1 to 128 experts, 1 to 1835 rows, K = 304 to 2256, 704
 // to 4096 weight rows).  Here: a base, and the workgroups two to a CU, each a fixed time
 // and its blocks.  There, while the tiles of 64 rows fit a round of the CUs: a stage a
-// block, one or two row fragments high, and the tiles' weights.  Measured, 8 rows | 32 rows
+// block, one or two row fragments high, and the tiles' weights.  Longer K and wider N than
+// fitted, measured afterwards at N = 4096, K = 7168 and N = 7168, K = 2048 (1, 32 and 256
+// experts, 1 to 256 rows): the faster kernel or one within 3% of it but once (32 rows over 32
+// experts, 142 us for 118).  Measured, 8 rows | 32 rows
 // | large kernel, us:
 //   1 expert, K = 2048, N = 1536: 8 rows 6.5 | 7.3 | 19.6; 128 14.2 | 8.2 | 24.1; 512 39.7 |
 //   15.9 | 24.3; 1000 72.4 | 25.8 | 24.7
@@ -228,6 +232,8 @@ static double few_tiles(double rows, int E, double h) {
 //   32 experts, K = 2256, N = 768: 22 rows 11.1 | 11.6 | 23.2; 467 29.9 | 19.9 | 27.3; 1835 79.7 | 34.5 | 32.1
 //   14 of 128 experts, a row each, N = 2048: K = 576 11.8 | 13.3 | 12.2, K = 1088 14.3 | 15.9 | 15.5;
 //   N = 4096, K = 1024 22.7 | 25.3 | 16.8
+//   8 of 256 experts, a row each: N = 4096, K = 7168, SwiGLU quantised 50.4 | 52.8 | 64.9 (235 MB of
+//   weights, 48 at the copy rate); N = 7168, K = 2048 33.0 | 36.7 | 28.5
 int blk_few_rows(int64_t rows, int E, int64_t N, int64_t K, int epilogue) {
   const double r = (double)rows, KB = (double)((K + FB - 1) / FB), nfr = (double)((N + 31) / 32);
   if (rows < 1) return 0;

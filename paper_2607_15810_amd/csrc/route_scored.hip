@@ -8,9 +8,13 @@
 // and then placed.
 //
 // 8192 tokens, 256 experts in 8 groups, k = 8 (8.4 MB of f32 logits, 2 us of HBM): choice
-// 17.5 us, counts 4.7, placing 6.3.  The choice is bound by its instructions: a wave per
-// token, four of a workgroup, k + 1 rounds of a 64-lane maximum each waiting for the last.
-// The gradient, 4096 x 128 in bf16: 5.8 us, float64 exponentials of the chosen.
+// 17.3 us, counts 4.3, placing 7.2.  The choice is bound by its vector instructions: 741 a
+// token, eight tokens a SIMD one after the other at 4 cycles and more each, 11.8 of the 17.3 us
+// (counters); beside them 238 scalar ones a token, the launch and the first loads.  No part
+// dominates: eight of the k + 1 rounds are 2 us, the float64 weights, on k of 64 lanes, 1.5,
+// the float64 choice of the doubtful 2.  The gradient, 4096 x 128 in bf16: 6.1 us, float64
+// exponentials of the chosen, one wave a token.  Placing adds the counts of all blocks in
+// every workgroup: the square of T / 256, which is small up to some 10^5 tokens.
 #include "fp8_block_dev.h"
 #include "route_scored_dev.h"
 
