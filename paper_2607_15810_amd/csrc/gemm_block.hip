@@ -33,7 +33,7 @@
 //    filled by direct global->LDS loads.
 //  * Bound, for hundreds of rows per expert, by the matrix unit and the vector unit beside
 //    it: 7 vector instructions per MFMA (decoding 3 to 4, rescaling 2), the matrix unit
-//    busy 50% of the cycles at 2.1 GHz (4096^3: 1.05 to 1.13 PFLOP/s by the box; an isolated
+//    busy 50% of the cycles at 2.1 GHz (4096^3: 1.05 to 1.13 PFLOP/s by the card; an isolated
 //    loop of the same instructions on random operands, which the chip's power limits, reaches
 //    1.5).  Of experts 0.73 to 0.8 PFLOP/s, busy 32 to 39%: tiles of uneven height (9 to 10
 //    vector instructions per MFMA), the epilogue, weights from HBM, and a stage's loads, which
